@@ -240,6 +240,91 @@ int jfa_jagged_softmax_backward(const void *y, const void *dy, const int64_t *of
                                 void *dx, void *stream);
 
 /*
+ * Linear attention with a decay for each head, on jagged tensors.  With g = exp(log_decay[h]), for every sample and head
+ *       S_i = g S_(i-1) + k_i^T v_i          (D x D, S_(-1) the initial state: element [d][e] belongs to k's d and v's e)
+ *       out_i = scale q_i S_i = scale (g^(i+1) q_i S_(-1) + sum_{j <= i} g^(i-j) (q_i . k_j) v_j)
+ * A sample's whole past is one D x D state a head: the causal sequence operator for histories that grow, event by event
+ * (jfa_linear_attention_step) or many events at a time (jfa_linear_attention with initial_state and final_state).
+ *
+ *   q, k, v, out, dout, dq, dk, dv   [sum_B, H, D], bf16, or fp32 for the _f32 variants; D in {32, 64, 128}
+ *   log_decay                        fp32 [H] on the device, at most 0; -inf is a decay of zero (a row then sees itself only)
+ *   initial_state, final_state, dfinal_state, dinitial_state   fp32 [B, H, D, D], each may be null: an initial state (a gradient of the
+ *                        final state) of zeros, a final state (a gradient of the initial state) that is not wanted.  A sample without rows
+ *                        hands its state through.
+ *   workspace            jfa_linear_attention_workspace_bytes(...) bytes of device memory, 16-byte aligned, that nobody else uses until
+ *                        the call's work is done; may be null where that is 0 (pass: 0 = forward, 1 = backward)
+ *
+ * Products are those of bf16 (or fp32) numbers with fp32 sums; the state is held in fp32.  In the bf16 calls the decayed products of rows up to
+ * 64 apart, and the state as a factor of out, are rounded to bf16 in front of their product; a final state (or a gradient of an initial
+ * one) is exact to fp32.  A row that is not finite reaches the other rows of its sample and head, earlier ones
+ * among them, and nothing else.  The gradient of log_decay is not computed.
+ * jfa_linear_attention_step takes one row per sequence, q, k, v, out [B, H, D], and a state [B, H, D, D]; new_state may be `state`.
+ * At most JFA_LINEAR_MAX_PAIRS samples times heads.  Everything else as for the calls above.
+ */
+#define JFA_LINEAR_MAX_PAIRS (1 << 22)
+size_t jfa_linear_attention_workspace_bytes(int64_t B, int64_t max_len, int H, int D, int pass);
+int jfa_linear_attention(const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len, int H,
+                         int D, float scale, const float *initial_state, void *out, float *final_state, void *workspace, size_t workspace_bytes,
+                         void *stream);
+int jfa_linear_attention_f32(const float *q, const float *k, const float *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len,
+                             int H, int D, float scale, const float *initial_state, float *out, float *final_state, void *workspace,
+                             size_t workspace_bytes, void *stream);
+int jfa_linear_attention_backward(const void *q, const void *k, const void *v, const void *dout, const float *log_decay, const int64_t *offsets, int64_t B,
+                                  int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state, void *dq, void *dk,
+                                  void *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream);
+int jfa_linear_attention_backward_f32(const float *q, const float *k, const float *v, const float *dout, const float *log_decay, const int64_t *offsets,
+                                      int64_t B, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state,
+                                      float *dq, float *dk, float *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream);
+int jfa_linear_attention_step(const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
+                              const float *state, void *out, float *new_state, void *stream);
+int jfa_linear_attention_step_f32(const float *q, const float *k, const float *v, const float *log_decay, int64_t B, int H, int D, float scale,
+                                  const float *state, float *out, float *new_state, void *stream);
+
+/*
+ * Row operators of a jagged tensor of `rows` rows, of which the first offsets[B] are there; the others are neither read nor written.
+ * offsets may be null (B is then not looked at): all rows are there.  Pointers need no more than their elements' alignment; rows
+ * that start on 16 bytes are moved 16 bytes at a time.  bf16, or fp32 for the _f32 variants.  At most JFA_ROWS_MAX rows (times reps) of at most
+ * JFA_ROW_ELEMENTS_MAX elements.
+ *
+ * Layer norm.  A row of the tensor holds `reps` rows of N elements (all heads of a row together: reps = 1, N = H D; each for itself: reps = H,
+ * N = D), each of which becomes
+ *       y = (x - mean) rstd weight + bias,   rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ *   x, y, dy, dx   [rows, reps, N];  weight, bias, dweight, dbias  [N], of x's type; each may be null: a weight of ones, a bias of zeros,
+ *                  a gradient that is not wanted
+ *   mean, rstd     fp32 [rows, reps]; may be null in the forward, what it wrote in the backward
+ *   dx = rstd (weight dy - mean(weight dy) - xh mean(weight dy xh)) with xh = (x - mean) rstd;
+ *   dweight = sum over all rows of dy xh, dbias = sum over all rows of dy, added in fp32 in an order that does not change.
+ *   workspace      jfa_layer_norm_workspace_bytes(rows, reps, N) bytes, 16-byte aligned, nobody else's until the call's work is done; may be
+ *                  null where neither dweight nor dbias is wanted
+ *
+ * Embedding lookup.  out[i] = scale table[ids[i]], zeros where ids[i] is not one of 0 .. V - 1.
+ *   table, dtable  [V, N];  ids  [rows], int64 or int32 (id_bytes 8 or 4);  out, dout  [rows, N]
+ *   dtable[v] = scale times the sum of dout[i] over the i with ids[i] = v, in fp32 and in an order that does not change; every row of it is written.
+ *   workspace      jfa_embedding_workspace_bytes(rows, V, N) bytes, 16-byte aligned, nobody else's until the call's work is done
+ */
+#define JFA_ROWS_MAX (1 << 30)
+#define JFA_ROW_ELEMENTS_MAX (1 << 20)
+size_t jfa_layer_norm_workspace_bytes(int64_t rows, int64_t reps, int64_t N);
+int jfa_layer_norm(const void *x, const void *weight, const void *bias, const int64_t *offsets, int64_t B, int64_t rows, int64_t reps, int64_t N, float eps,
+                   void *y, float *mean, float *rstd, void *stream);
+int jfa_layer_norm_f32(const float *x, const float *weight, const float *bias, const int64_t *offsets, int64_t B, int64_t rows, int64_t reps, int64_t N,
+                       float eps, float *y, float *mean, float *rstd, void *stream);
+int jfa_layer_norm_backward(const void *x, const void *weight, const void *dy, const float *mean, const float *rstd, const int64_t *offsets, int64_t B,
+                            int64_t rows, int64_t reps, int64_t N, void *dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+int jfa_layer_norm_backward_f32(const float *x, const float *weight, const float *dy, const float *mean, const float *rstd, const int64_t *offsets, int64_t B,
+                                int64_t rows, int64_t reps, int64_t N, float *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                                void *stream);
+size_t jfa_embedding_workspace_bytes(int64_t rows, int64_t V, int64_t N);
+int jfa_embedding(const void *table, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale,
+                  void *out, void *stream);
+int jfa_embedding_f32(const float *table, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale,
+                      float *out, void *stream);
+int jfa_embedding_backward(const void *dout, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale,
+                           void *dtable, void *workspace, size_t workspace_bytes, void *stream);
+int jfa_embedding_backward_f32(const float *dout, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N,
+                               float scale, float *dtable, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * The offsets-driven work schedule on its own (the first kernel of the attention calls on all but
  * small problems, which build it in the attention kernel), for inspection and tests.  For row blocks of block_rows rows it writes, on the device,
  *   order      int32 [B]    sample ids, samples with more row blocks first

@@ -8,9 +8,12 @@ step on a small batch spends half as much host time in; the torch.autograd.Funct
 
     out = jagged_flash_attention(q, k, v, offsets, max_len)                      # self attention, causal=True for the causal variant
     out = jagged_flash_cross_attention(q, k, v, offsets_q, offsets_kv, max_len_q, max_len_kv)
+    out = jagged_linear_attention(q, k, v, log_decay, offsets, max_len)              # a decay for each head; states in and out if wanted
+    y = jagged_layer_norm(x, weight, bias, offsets)                                  # rows of any shape that ends in weight's
+    x = jagged_embedding(table, ids, offsets, scale)                                 # a row of the table for each id
 
 q, k, v: [rows, H, D] bf16 or fp32 on the GPU, contiguous; offsets: int64 [B + 1] on the GPU.  Gradients flow to q, k
-and v; offsets and the length bounds are not differentiable.
+and v (and to x, weight, bias, the table and the states); offsets, ids, decays and the length bounds are not differentiable.
 """
 import ctypes
 import importlib.util
@@ -23,7 +26,7 @@ from torch.autograd import forward_ad
 from . import binding
 from .build import native_path
 
-__all__ = ["jagged_flash_attention", "jagged_flash_cross_attention"]
+__all__ = ["jagged_flash_attention", "jagged_flash_cross_attention", "jagged_linear_attention", "jagged_layer_norm", "jagged_embedding"]
 
 
 class _SelfAttention(torch.autograd.Function):
@@ -55,6 +58,65 @@ class _CrossAttention(torch.autograd.Function):
         dq, dk, dv, _ = binding.jfa_backward_cross(q, k, v, out, dout.contiguous(), lse, offsets_q, offsets_kv,
                                                    ctx.max_len_q, ctx.max_len_kv)
         return dq, dk, dv, None, None, None, None
+
+
+def _check_capture():
+    """In a backward: refuses a capture that would end the process (see gradients_leave_capture in csrc/jfa_autograd.cpp)."""
+    if torch.cuda.is_current_stream_capturing():
+        if _native is None:
+            _load_native()
+        if _native is not False and _native.gradients_leave_capture():
+            raise RuntimeError("A backward pass is being captured into a graph while the gradients of its leaves belong to another stream: an earlier graph of the "
+                               "same leaves is still alive.  Let go of that graph's results first, or run it on the stream of the capture.")
+
+
+class _LinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, offsets, max_len, scale, initial_state, return_state):
+        out, final_state = binding.jfa_linear_attention(q, k, v, log_decay, offsets, max_len, scale, initial_state, return_state=return_state)
+        ctx.save_for_backward(q, k, v, log_decay, offsets, initial_state)
+        ctx.max_len, ctx.scale = max_len, scale
+        return (out, final_state) if return_state else out
+
+    @staticmethod
+    def backward(ctx, dout, dfinal_state=None):
+        _check_capture()
+        q, k, v, log_decay, offsets, initial_state = ctx.saved_tensors
+        dq, dk, dv, dinitial = binding.jfa_linear_attention_backward(
+            q, k, v, dout.contiguous(), log_decay, offsets, ctx.max_len, ctx.scale, initial_state,
+            None if dfinal_state is None else dfinal_state.contiguous(), return_dstate=ctx.needs_input_grad[7])
+        return dq, dk, dv, None, None, None, None, dinitial, None
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, offsets, eps):
+        y, mean, rstd = binding.jfa_layer_norm(x, weight, bias, offsets, eps, statistics=any(ctx.needs_input_grad))
+        ctx.save_for_backward(x, weight, mean, rstd, offsets)
+        ctx.shape = next((t.shape for t in (weight, bias) if t is not None), x.shape[-1:])
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        _check_capture()
+        x, weight, mean, rstd, offsets = ctx.saved_tensors
+        dx, dweight, dbias = binding.jfa_layer_norm_backward(x, weight, dy.contiguous(), mean, rstd, offsets, normalized_shape=ctx.shape,
+                                                             want_dweight=ctx.needs_input_grad[1], want_dbias=ctx.needs_input_grad[2])
+        return dx, dweight, dbias, None, None
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, offsets, scale):
+        ctx.save_for_backward(ids, offsets)
+        ctx.V, ctx.scale = table.shape[0], scale
+        return binding.jfa_embedding(table, ids, offsets, scale)
+
+    @staticmethod
+    def backward(ctx, dout):
+        _check_capture()
+        ids, offsets = ctx.saved_tensors
+        return binding.jfa_embedding_backward(dout.contiguous(), ids, ctx.V, offsets, ctx.scale), None, None, None
 
 
 _native = None   # the C++ nodes; False where they have not been built for this torch
@@ -109,3 +171,24 @@ def jagged_flash_cross_attention(q, k, v, offsets_q, offsets_kv, max_len_q: int,
         if out is not None:
             return out
     return _CrossAttention.apply(q, k, v, offsets_q, offsets_kv, max_len_q, max_len_kv)
+
+
+def jagged_linear_attention(q, k, v, log_decay, offsets, max_len: int, scale=None, initial_state=None, return_state: bool = False):
+    """out_i = scale q_i S_i with S_i = exp(log_decay) S_(i-1) + k_i^T v_i per sample and head; q, k, v as for jagged_flash_attention,
+    log_decay fp32 [H], scale 1 / sqrt(D) if not given.  initial_state: fp32 [B, H, D, D], zeros if not given; return_state: the samples'
+    final states too, as a second result.  Gradients flow to the states as well, not to log_decay."""
+    if log_decay.requires_grad:
+        raise ValueError("jagged_linear_attention: log_decay is not differentiable")
+    return _LinearAttention.apply(q, k, v, log_decay, offsets, int(max_len), q.shape[-1] ** -0.5 if scale is None else float(scale), initial_state, bool(return_state))
+
+
+def jagged_layer_norm(x, weight=None, bias=None, offsets=None, eps: float = 1e-5):
+    """Layer norm over the last dimensions of x [rows, ...], those of weight and bias (without either the last one).  offsets: of
+    the rows only the first offsets[B] are there."""
+    return _LayerNorm.apply(x, weight, bias, offsets, float(eps))
+
+
+def jagged_embedding(table, ids, offsets=None, scale: float = 1.0):
+    """scale table[ids] for table [V, ...] and ids [rows] (int64 or int32), zeros for an id outside the table.  offsets: of the
+    rows only the first offsets[B] are there."""
+    return _Embedding.apply(table, ids, offsets, float(scale))

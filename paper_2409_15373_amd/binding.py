@@ -6,6 +6,7 @@ CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -32,6 +33,10 @@ EXPORTS = (
     "jfa_backward_cross", "jfa_backward_cross_f32", "jfa_forward_causal", "jfa_forward_causal_f32",
     "jfa_backward_causal", "jfa_backward_causal_f32", "jfa_unfused_product", "jfa_unfused_softmax_backward",
     "jfa_unfused_apply_transposed", "jfa_forward_noalloc",
+    "jfa_linear_attention", "jfa_linear_attention_f32", "jfa_linear_attention_backward", "jfa_linear_attention_backward_f32",
+    "jfa_linear_attention_step", "jfa_linear_attention_step_f32", "jfa_linear_attention_workspace_bytes",
+    "jfa_layer_norm", "jfa_layer_norm_f32", "jfa_layer_norm_backward", "jfa_layer_norm_backward_f32", "jfa_layer_norm_workspace_bytes",
+    "jfa_embedding", "jfa_embedding_f32", "jfa_embedding_backward", "jfa_embedding_backward_f32", "jfa_embedding_workspace_bytes",
 )
 
 
@@ -114,6 +119,24 @@ def load() -> ctypes.CDLL:
     lib.jfa_jagged_softmax.argtypes = [vp, vp, i64, i64, i32, vp, vp]
     lib.jfa_jagged_softmax_backward.restype = i32
     lib.jfa_jagged_softmax_backward.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp]
+    f32 = ctypes.c_float
+    for name, restype, argtypes in (
+            ("jfa_linear_attention", i32, [vp] * 5 + [i64, i64, i32, i32, f32] + [vp] * 4 + [sz, vp]),
+            ("jfa_linear_attention_backward", i32, [vp] * 6 + [i64, i64, i32, i32, f32] + [vp] * 7 + [sz, vp]),
+            ("jfa_linear_attention_step", i32, [vp] * 4 + [i64, i32, i32, f32] + [vp] * 4),
+            ("jfa_layer_norm", i32, [vp] * 4 + [i64] * 4 + [f32] + [vp] * 4),
+            ("jfa_layer_norm_backward", i32, [vp] * 6 + [i64] * 4 + [vp] * 4 + [sz, vp]),
+            ("jfa_embedding", i32, [vp, vp, i32, vp] + [i64] * 4 + [f32, vp, vp]),
+            ("jfa_embedding_backward", i32, [vp, vp, i32, vp] + [i64] * 4 + [f32, vp, vp, sz, vp])):
+        for suffix in ("", "_f32"):
+            getattr(lib, name + suffix).restype = restype
+            getattr(lib, name + suffix).argtypes = argtypes
+    lib.jfa_linear_attention_workspace_bytes.restype = sz
+    lib.jfa_linear_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32]
+    lib.jfa_layer_norm_workspace_bytes.restype = sz
+    lib.jfa_layer_norm_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.jfa_embedding_workspace_bytes.restype = sz
+    lib.jfa_embedding_workspace_bytes.argtypes = [i64, i64, i64]
     _lib = lib
     return lib
 
@@ -409,6 +432,156 @@ def jfa_jagged_softmax_backward(y: torch.Tensor, dy: torch.Tensor, offsets: torc
     _check(load().jfa_jagged_softmax_backward(_ptr(y), _ptr(dy), _ptr(offsets), offsets.numel() - 1, max_len, y.shape[1],
                                               _ptr(dx), _stream()))
     return dx
+
+
+# ---- sequence operators: linear attention, layer norm, embedding lookup ----
+
+def _on_device_of(first: torch.Tensor, *others: Optional[torch.Tensor]):
+    """The device that a call's tensors share, made the current one (the library works on the current device)."""
+    assert first.is_cuda and all(t is None or t.device == first.device for t in others), "tensors of one GPU only"
+    if _current_device is not None and _current_device() == first.device.index:
+        return contextlib.nullcontext()
+    return torch.cuda.device(first.device)
+
+
+def _workspace(n_bytes: int, device) -> Optional[torch.Tensor]:
+    return torch.empty(n_bytes, dtype=torch.uint8, device=device) if n_bytes else None
+
+
+def _check_linear(q, k, v, log_decay, batch: Optional[int], *states):
+    assert q.dim() == 3 and k.shape == q.shape and v.shape == q.shape and k.dtype == q.dtype and v.dtype == q.dtype
+    _, H, D = q.shape
+    assert log_decay.dtype == torch.float32 and log_decay.shape == (H,), "log_decay: fp32 [H]"
+    for state in states:
+        assert state is None or (state.dtype == torch.float32 and state.shape == (batch, H, D, D)), "states: fp32 [B, H, D, D]"
+
+
+def _check_offsets_tensor(offsets) -> int:
+    assert offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.numel() >= 1
+    return offsets.numel() - 1
+
+
+def jfa_linear_attention(q, k, v, log_decay, offsets, max_len: int, scale: Optional[float] = None, initial_state=None, out=None, final_state=None,
+                         return_state: bool = False) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """out [sum_B, H, D] and, if asked for (return_state, or a tensor to write it to), the samples' final states fp32 [B, H, D, D].
+    scale: 1 / sqrt(D) if not given."""
+    B = _check_offsets_tensor(offsets)
+    _check_linear(q, k, v, log_decay, B, initial_state, final_state)
+    assert out is None or (out.shape == q.shape and out.dtype == q.dtype)
+    _, H, D = q.shape
+    with _on_device_of(q, k, v, log_decay, offsets, initial_state, out, final_state):
+        out = torch.empty_like(q) if out is None else out
+        if final_state is None and return_state:
+            final_state = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
+        workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, max_len, H, D, 0), q.device)
+        _check(_pick(q.dtype, "jfa_linear_attention")(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale, _ptr(initial_state), _ptr(out),
+            _ptr(final_state), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return out, final_state
+
+
+def jfa_linear_attention_backward(q, k, v, dout, log_decay, offsets, max_len: int, scale: Optional[float] = None, initial_state=None, dfinal_state=None,
+                                  dq=None, dk=None, dv=None, dinitial_state=None, return_dstate: bool = False):
+    """dq, dk, dv [sum_B, H, D] and, if asked for, the gradient of the initial states fp32 [B, H, D, D]."""
+    B = _check_offsets_tensor(offsets)
+    _check_linear(q, k, v, log_decay, B, initial_state, dfinal_state, dinitial_state)
+    assert all(t is None or (t.shape == q.shape and t.dtype == q.dtype) for t in (dout, dq, dk, dv))
+    _, H, D = q.shape
+    with _on_device_of(q, k, v, dout, log_decay, offsets, initial_state, dfinal_state, dq, dk, dv, dinitial_state):
+        dq, dk, dv = (torch.empty_like(q) if t is None else t for t in (dq, dk, dv))
+        if dinitial_state is None and return_dstate:
+            dinitial_state = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
+        workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, max_len, H, D, 1), q.device)
+        _check(_pick(q.dtype, "jfa_linear_attention_backward")(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale, _ptr(initial_state),
+            _ptr(dfinal_state), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dinitial_state), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return dq, dk, dv, dinitial_state
+
+
+def jfa_linear_attention_step(q, k, v, log_decay, state, scale: Optional[float] = None, out=None, new_state=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """One row per sequence: q, k, v, out [B, H, D]; the state fp32 [B, H, D, D] is updated in place unless new_state is given.
+    scale: 1 / sqrt(D) if not given."""
+    B, H, D = q.shape
+    new_state = state if new_state is None else new_state
+    _check_linear(q, k, v, log_decay, B, state, new_state)
+    assert out is None or (out.shape == q.shape and out.dtype == q.dtype)
+    with _on_device_of(q, k, v, log_decay, state, out, new_state):
+        out = torch.empty_like(q) if out is None else out
+        _check(_pick(q.dtype, "jfa_linear_attention_step")(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), B, H, D, D ** -0.5 if scale is None else scale, _ptr(state),
+                                                           _ptr(out), _ptr(new_state), _stream()))
+    return out, new_state
+
+
+def _norm_sizes(x, weight, bias, offsets):
+    """(rows, reps, N, B): x [rows, ...] whose last dimensions are weight's (or bias's; without either only the last)."""
+    shape = next((t.shape for t in (weight, bias) if t is not None), x.shape[-1:])
+    assert x.dim() >= 1 + len(shape) and len(shape) >= 1 and x.shape[x.dim() - len(shape):] == shape, "weight and bias: x's last dimensions"
+    assert all(t is None or (t.shape == shape and t.dtype == x.dtype) for t in (weight, bias)), "weight and bias: of one shape, and of x's type"
+    N = shape.numel()
+    return x.shape[0], x.shape[1:].numel() // N if N else 1, N, 0 if offsets is None else _check_offsets_tensor(offsets)
+
+
+def jfa_layer_norm(x, weight=None, bias=None, offsets=None, eps: float = 1e-5, y=None, statistics: bool = True):
+    """y like x, and mean and rstd fp32 [rows, reps] (None where `statistics` is false).  x [rows, ...]; weight and bias have the shape of
+    the dimensions that are normalised, x's last ones; with offsets only the first offsets[B] rows are there."""
+    rows, reps, N, B = _norm_sizes(x, weight, bias, offsets)
+    assert y is None or (y.shape == x.shape and y.dtype == x.dtype)
+    with _on_device_of(x, weight, bias, offsets, y):
+        y = torch.empty_like(x) if y is None else y
+        mean = rstd = None
+        if statistics:
+            mean, rstd = torch.empty((2, rows, reps), dtype=torch.float32, device=x.device).unbind()
+        _check(_pick(x.dtype, "jfa_layer_norm")(_ptr(x), _ptr(weight), _ptr(bias), _ptr(offsets), B, rows, reps, N, eps, _ptr(y), _ptr(mean), _ptr(rstd), _stream()))
+    return y, mean, rstd
+
+
+def jfa_layer_norm_backward(x, weight, dy, mean, rstd, offsets=None, dx=None, dweight=None, dbias=None, normalized_shape=None, want_dweight: bool = True,
+                            want_dbias: bool = True):
+    """dx like x, dweight and dbias of weight's shape (None where not wanted).  normalized_shape: for a layer norm without weight."""
+    shape = weight.shape if weight is not None else torch.Size(x.shape[-1:] if normalized_shape is None else normalized_shape)
+    rows, reps, N, B = _norm_sizes(x, torch.empty(shape, dtype=x.dtype, device="meta"), None, offsets)
+    assert dy.shape == x.shape and dy.dtype == x.dtype and (dx is None or (dx.shape == x.shape and dx.dtype == x.dtype))
+    assert all(t.dtype == torch.float32 and t.numel() == rows * reps for t in (mean, rstd)), "mean and rstd: fp32 [rows, reps]"
+    assert all(t is None or (t.shape == shape and t.dtype == x.dtype) for t in (weight, dweight, dbias))
+    with _on_device_of(x, weight, dy, mean, rstd, offsets, dx, dweight, dbias):
+        dx = torch.empty_like(x) if dx is None else dx
+        dweight = torch.empty(shape, dtype=x.dtype, device=x.device) if dweight is None and want_dweight else dweight
+        dbias = torch.empty(shape, dtype=x.dtype, device=x.device) if dbias is None and want_dbias else dbias
+        workspace = None if dweight is None and dbias is None else _workspace(load().jfa_layer_norm_workspace_bytes(rows, reps, N), x.device)
+        _check(_pick(x.dtype, "jfa_layer_norm_backward")(
+            _ptr(x), _ptr(weight), _ptr(dy), _ptr(mean), _ptr(rstd), _ptr(offsets), B, rows, reps, N, _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+            0 if workspace is None else workspace.numel(), _stream()))
+    return dx, dweight, dbias
+
+
+def _embedding_sizes(ids, offsets):
+    assert ids.dim() == 1 and ids.dtype in (torch.int64, torch.int32), "ids: int64 or int32, one per row"
+    return ids.numel(), ids.element_size(), 0 if offsets is None else _check_offsets_tensor(offsets)
+
+
+def jfa_embedding(table, ids, offsets=None, scale: float = 1.0, out=None):
+    """out [rows, ...] = scale table[ids] for table [V, ...] and ids [rows], zeros for ids outside the table; with offsets only the first
+    offsets[B] rows are there."""
+    rows, id_bytes, B = _embedding_sizes(ids, offsets)
+    V, shape = table.shape[0], table.shape[1:]
+    assert out is None or (out.shape == (rows,) + tuple(shape) and out.dtype == table.dtype)
+    with _on_device_of(table, ids, offsets, out):
+        out = torch.empty((rows,) + tuple(shape), dtype=table.dtype, device=table.device) if out is None else out
+        _check(_pick(table.dtype, "jfa_embedding")(_ptr(table), _ptr(ids), id_bytes, _ptr(offsets), B, rows, V, shape.numel(), scale, _ptr(out), _stream()))
+    return out
+
+
+def jfa_embedding_backward(dout, ids, V: int, offsets=None, scale: float = 1.0, dtable=None):
+    """dtable [V, ...], every row of it: scale times the sum of the dout [rows, ...] of its ids, added in the order of the rows."""
+    rows, id_bytes, B = _embedding_sizes(ids, offsets)
+    shape = dout.shape[1:]
+    assert dout.shape[0] == rows and (dtable is None or (dtable.shape == (V,) + tuple(shape) and dtable.dtype == dout.dtype))
+    with _on_device_of(dout, ids, offsets, dtable):
+        dtable = torch.empty((V,) + tuple(shape), dtype=dout.dtype, device=dout.device) if dtable is None else dtable
+        workspace = _workspace(load().jfa_embedding_workspace_bytes(rows, V, shape.numel()), dout.device)
+        _check(_pick(dout.dtype, "jfa_embedding_backward")(_ptr(dout), _ptr(ids), id_bytes, _ptr(offsets), B, rows, V, shape.numel(), scale, _ptr(dtable),
+                                                           _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return dtable
 
 
 def jfa_check_offsets(offsets: torch.Tensor, max_len: int) -> int:

@@ -1,5 +1,6 @@
 // extern "C" entry points of libjfa.so: argument validation, the private work table and the
 // sequence of kernel launches of each call.  See include/jfa.h for the contract.
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <stdarg.h>
@@ -802,6 +803,261 @@ int jfa_jagged_softmax_backward(const void *y, const void *dy, const int64_t *of
     { ScopedTimer tm("jagged_softmax_bwd", s); e = jfa::launch_jagged_softmax(true, y, dy, offsets, (int)B, max_len, D, v.counters, dx, v.cus, s); }
     if (e != hipSuccess) return hip_fail("jagged_softmax backward kernel", e);
     return JFA_OK;
+}
+
+// ---- linear attention with a decay for each head ----
+
+namespace {
+int linear_begin(const char *who, int64_t B, int64_t max_len, int H, int D) {
+    if (B < 0) return fail(JFA_ERR_INVALID_ARG, "%s: B = %lld is negative", who, (long long)B);
+    if (max_len < 0 || max_len >= (int64_t)1 << 31) return fail(JFA_ERR_INVALID_ARG, "%s: bad max_len = %lld", who, (long long)max_len);
+    if (H <= 0) return fail(JFA_ERR_INVALID_ARG, "%s: H = %d must be positive", who, H);
+    if (D != 32 && D != 64 && D != 128) return fail(JFA_ERR_UNSUPPORTED, "%s: D = %d is not one of 32, 64, 128", who, D);
+    if (B > JFA_LINEAR_MAX_PAIRS / H) return fail(JFA_ERR_UNSUPPORTED, "%s: B * H = %lld * %d exceeds %d", who, (long long)B, H, JFA_LINEAR_MAX_PAIRS);
+    return JFA_OK;
+}
+int linear_pointers(const char *who, const void *const *tensors, int n, const float *const *optional, int n_optional) {
+    for (int i = 0; i < n; ++i) {
+        if (!tensors[i]) return fail(JFA_ERR_INVALID_ARG, "%s: pointer argument %d is null", who, i);
+        if (misaligned(tensors[i])) return fail(JFA_ERR_INVALID_ARG, "%s: pointer argument %d is not 16-byte aligned", who, i);
+    }
+    for (int i = 0; i < n_optional; ++i)
+        if (misaligned(optional[i])) return fail(JFA_ERR_INVALID_ARG, "%s: a state is not 16-byte aligned", who);
+    return JFA_OK;
+}
+size_t linear_workspace(int64_t B, int64_t max_len, int H, int D, int walks, int *segments, int *segment_rows) {
+    *segment_rows = jfa::linear_segment_rows(B, max_len, H, walks, jfa::kLinearCus);
+    *segments = max_len > *segment_rows ? (int)((max_len + *segment_rows - 1) / *segment_rows) : 1;
+    return (size_t)(walks * B * H * (*segments - 1)) * D * D * sizeof(float);
+}
+int linear_launch(const char *who, bool f32, const jfa::LinearWalks &walks, int n_walks, bool states, const float *log_decay, const int64_t *offsets,
+                  int64_t B, int64_t max_len, int H, int D, void *workspace, size_t workspace_bytes, hipStream_t s) {
+    int segments, segment_rows;
+    const size_t need = linear_workspace(B, max_len, H, D, n_walks, &segments, &segment_rows);
+    if (workspace_bytes < need || (need && !workspace))
+        return fail(JFA_ERR_INVALID_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : 0, need);
+    if (need && misaligned(workspace)) return fail(JFA_ERR_INVALID_ARG, "%s: the workspace is not 16-byte aligned", who);
+    ScopedTimer tm(n_walks == 1 ? "linear_attention" : "linear_attention_bwd", s);
+    const hipError_t e = jfa::launch_linear_walks(f32, walks, n_walks, states, log_decay, offsets, B, H, D, segments, segment_rows, (float *)workspace, s);
+    return e == hipSuccess ? JFA_OK : hip_fail("linear attention kernel", e);
+}
+int linear_forward(const char *who, bool f32, const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B,
+                   int64_t max_len, int H, int D, float scale, const float *initial_state, void *out, float *final_state, void *workspace,
+                   size_t workspace_bytes, hipStream_t s) {
+    int st = linear_begin(who, B, max_len, H, D);
+    if (st != JFA_OK || B == 0) return st;
+    const void *tensors[] = {q, k, v, out, offsets, log_decay};
+    const float *states[] = {initial_state, final_state};
+    if ((st = linear_pointers(who, tensors, 6, states, 2)) != JFA_OK) return st;
+    const jfa::LinearWalks walks{{{q, k, v, out, initial_state, final_state, 1.0f, scale, false, false}}};
+    return linear_launch(who, f32, walks, 1, final_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
+}
+int linear_backward(const char *who, bool f32, const void *q, const void *k, const void *v, const void *dout, const float *log_decay,
+                    const int64_t *offsets, int64_t B, int64_t max_len, int H, int D, float scale, const float *initial_state,
+                    const float *dfinal_state, void *dq, void *dk, void *dv, float *dinitial_state, void *workspace, size_t workspace_bytes,
+                    hipStream_t s) {
+    int st = linear_begin(who, B, max_len, H, D);
+    if (st != JFA_OK || B == 0) return st;
+    const void *tensors[] = {q, k, v, dout, dq, dk, dv, offsets, log_decay};
+    const float *states[] = {initial_state, dfinal_state, dinitial_state};
+    if ((st = linear_pointers(who, tensors, 9, states, 3)) != JFA_OK) return st;
+    const jfa::LinearWalks walks{{{dout, v, k, dq, initial_state, nullptr, 1.0f, scale, false, true},
+                                  {v, dout, q, dk, dfinal_state, nullptr, scale, 1.0f, true, true},
+                                  {k, q, dout, dv, dfinal_state, dinitial_state, scale, 1.0f, true, false}}};
+    return linear_launch(who, f32, walks, 3, dinitial_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
+}
+int linear_step(const char *who, bool f32, const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
+                const float *state, void *out, float *new_state, hipStream_t s) {
+    int st = linear_begin(who, B, 1, H, D);
+    if (st != JFA_OK || B == 0) return st;
+    const void *tensors[] = {q, k, v, out, state, new_state, log_decay};
+    if ((st = linear_pointers(who, tensors, 7, nullptr, 0)) != JFA_OK) return st;
+    ScopedTimer tm("linear_attention_step", s);
+    const hipError_t e = jfa::launch_linear_step(f32, q, k, v, log_decay, B, H, D, scale, state, out, new_state, s);
+    return e == hipSuccess ? JFA_OK : hip_fail("linear attention step kernel", e);
+}
+}  // namespace
+
+size_t jfa_linear_attention_workspace_bytes(int64_t B, int64_t max_len, int H, int D, int pass) {
+    if (linear_begin("jfa_linear_attention_workspace_bytes", B, max_len, H, D) != JFA_OK || B == 0) return 0;
+    int segments, segment_rows;
+    return linear_workspace(B, max_len, H, D, pass ? 3 : 1, &segments, &segment_rows);
+}
+int jfa_linear_attention(const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len, int H,
+                         int D, float scale, const float *initial_state, void *out, float *final_state, void *workspace, size_t workspace_bytes,
+                         void *stream) {
+    return linear_forward("jfa_linear_attention", false, q, k, v, log_decay, offsets, B, max_len, H, D, scale, initial_state, out, final_state, workspace,
+                          workspace_bytes, (hipStream_t)stream);
+}
+int jfa_linear_attention_f32(const float *q, const float *k, const float *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len,
+                             int H, int D, float scale, const float *initial_state, float *out, float *final_state, void *workspace,
+                             size_t workspace_bytes, void *stream) {
+    return linear_forward("jfa_linear_attention_f32", true, q, k, v, log_decay, offsets, B, max_len, H, D, scale, initial_state, out, final_state, workspace,
+                          workspace_bytes, (hipStream_t)stream);
+}
+int jfa_linear_attention_backward(const void *q, const void *k, const void *v, const void *dout, const float *log_decay, const int64_t *offsets, int64_t B,
+                                  int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state, void *dq, void *dk,
+                                  void *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream) {
+    return linear_backward("jfa_linear_attention_backward", false, q, k, v, dout, log_decay, offsets, B, max_len, H, D, scale, initial_state, dfinal_state, dq,
+                           dk, dv, dinitial_state, workspace, workspace_bytes, (hipStream_t)stream);
+}
+int jfa_linear_attention_backward_f32(const float *q, const float *k, const float *v, const float *dout, const float *log_decay, const int64_t *offsets,
+                                      int64_t B, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state,
+                                      float *dq, float *dk, float *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream) {
+    return linear_backward("jfa_linear_attention_backward_f32", true, q, k, v, dout, log_decay, offsets, B, max_len, H, D, scale, initial_state, dfinal_state,
+                           dq, dk, dv, dinitial_state, workspace, workspace_bytes, (hipStream_t)stream);
+}
+int jfa_linear_attention_step(const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
+                              const float *state, void *out, float *new_state, void *stream) {
+    return linear_step("jfa_linear_attention_step", false, q, k, v, log_decay, B, H, D, scale, state, out, new_state, (hipStream_t)stream);
+}
+int jfa_linear_attention_step_f32(const float *q, const float *k, const float *v, const float *log_decay, int64_t B, int H, int D, float scale,
+                                  const float *state, float *out, float *new_state, void *stream) {
+    return linear_step("jfa_linear_attention_step_f32", true, q, k, v, log_decay, B, H, D, scale, state, out, new_state, (hipStream_t)stream);
+}
+
+// ---- layer norm ----
+
+namespace {
+int rows_begin(const char *who, const int64_t *offsets, int64_t B, int64_t rows, int64_t N) {
+    if (rows < 0 || rows > JFA_ROWS_MAX) return fail(rows < 0 ? JFA_ERR_INVALID_ARG : JFA_ERR_UNSUPPORTED, "%s: bad rows = %lld", who, (long long)rows);
+    if (N <= 0 || N > JFA_ROW_ELEMENTS_MAX)
+        return fail(N <= 0 ? JFA_ERR_INVALID_ARG : JFA_ERR_UNSUPPORTED, "%s: N = %lld is not one of 1 .. %d", who, (long long)N, JFA_ROW_ELEMENTS_MAX);
+    if (offsets && (B < 0 || B >= (int64_t)1 << 30)) return fail(JFA_ERR_INVALID_ARG, "%s: bad B = %lld", who, (long long)B);
+    return JFA_OK;
+}
+// Element-wise access is what every pointer has to allow; 16-byte alignment of rows is made use of where it is given.
+int rows_pointer(const char *who, const char *name, const void *p, size_t alignment, bool needed) {
+    if (!p) return needed ? fail(JFA_ERR_INVALID_ARG, "%s: %s is null", who, name) : JFA_OK;
+    if ((uintptr_t)p % alignment) return fail(JFA_ERR_INVALID_ARG, "%s: %s is not aligned to its elements", who, name);
+    return JFA_OK;
+}
+struct RowsPointer { const char *name; const void *p; size_t alignment; bool needed; };
+int rows_pointers(const char *who, std::initializer_list<RowsPointer> pointers) {
+    for (const RowsPointer &x : pointers)
+        if (const int st = rows_pointer(who, x.name, x.p, x.alignment, x.needed)) return st;
+    return JFA_OK;
+}
+int check_reps(const char *who, int64_t rows, int64_t reps) {
+    if (reps <= 0 || (rows > 0 && reps > JFA_ROWS_MAX / rows)) return fail(JFA_ERR_INVALID_ARG, "%s: bad reps = %lld", who, (long long)reps);
+    return JFA_OK;
+}
+int norm_forward(const char *who, bool f32, const void *x, const void *weight, const void *bias, const int64_t *offsets, int64_t B, int64_t rows, int64_t reps,
+                 int64_t N, float eps, void *y, float *mean, float *rstd, hipStream_t s) {
+    int st = rows_begin(who, offsets, B, rows, N);
+    if (st == JFA_OK) st = check_reps(who, rows, reps);
+    if (st != JFA_OK || rows == 0) return st;
+    const size_t size = f32 ? 4 : 2;
+    st = rows_pointers(who, {{"x", x, size, true}, {"y", y, size, true}, {"weight", weight, size, false}, {"bias", bias, size, false}, {"offsets", offsets, 8, false},
+                             {"mean", mean, 4, false}, {"rstd", rstd, 4, false}});
+    if (st != JFA_OK) return st;
+    ScopedTimer tm("layer_norm", s);
+    const hipError_t e = jfa::launch_layer_norm(f32, x, weight, bias, offsets, B, rows, reps, N, eps, y, mean, rstd, s);
+    return e == hipSuccess ? JFA_OK : hip_fail("layer norm kernel", e);
+}
+int norm_backward(const char *who, bool f32, const void *x, const void *weight, const void *dy, const float *mean, const float *rstd, const int64_t *offsets,
+                  int64_t B, int64_t rows, int64_t reps, int64_t N, void *dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, hipStream_t s) {
+    int st = rows_begin(who, offsets, B, rows, N);
+    if (st == JFA_OK) st = check_reps(who, rows, reps);
+    if (st != JFA_OK || (rows == 0 && !dweight && !dbias)) return st;
+    const size_t size = f32 ? 4 : 2;
+    const bool some = rows > 0;
+    st = rows_pointers(who, {{"x", x, size, some}, {"dy", dy, size, some}, {"mean", mean, 4, some}, {"rstd", rstd, 4, some}, {"dx", dx, size, some},
+                             {"weight", weight, size, false}, {"dweight", dweight, size, false}, {"dbias", dbias, size, false}, {"offsets", offsets, 8, false}});
+    if (st != JFA_OK) return st;
+    const size_t need = dweight || dbias ? jfa::layer_norm_workspace(rows * reps, N) : 0;
+    if (workspace_bytes < need || (need && !workspace))
+        return fail(JFA_ERR_INVALID_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : 0, need);
+    if (need && misaligned(workspace)) return fail(JFA_ERR_INVALID_ARG, "%s: the workspace is not 16-byte aligned", who);
+    ScopedTimer tm("layer_norm_bwd", s);
+    const hipError_t e = jfa::launch_layer_norm_backward(f32, x, weight, dy, mean, rstd, offsets, B, rows, reps, N, dx, dweight, dbias, workspace, s);
+    return e == hipSuccess ? JFA_OK : hip_fail("layer norm backward kernel", e);
+}
+}  // namespace
+
+size_t jfa_layer_norm_workspace_bytes(int64_t rows, int64_t reps, int64_t N) {
+    if (rows_begin("jfa_layer_norm_workspace_bytes", nullptr, 0, rows, N) != JFA_OK || check_reps("jfa_layer_norm_workspace_bytes", rows, reps) != JFA_OK) return 0;
+    return jfa::layer_norm_workspace(rows * reps, N);
+}
+int jfa_layer_norm(const void *x, const void *weight, const void *bias, const int64_t *offsets, int64_t B, int64_t rows, int64_t reps, int64_t N, float eps,
+                   void *y, float *mean, float *rstd, void *stream) {
+    return norm_forward("jfa_layer_norm", false, x, weight, bias, offsets, B, rows, reps, N, eps, y, mean, rstd, (hipStream_t)stream);
+}
+int jfa_layer_norm_f32(const float *x, const float *weight, const float *bias, const int64_t *offsets, int64_t B, int64_t rows, int64_t reps, int64_t N,
+                       float eps, float *y, float *mean, float *rstd, void *stream) {
+    return norm_forward("jfa_layer_norm_f32", true, x, weight, bias, offsets, B, rows, reps, N, eps, y, mean, rstd, (hipStream_t)stream);
+}
+int jfa_layer_norm_backward(const void *x, const void *weight, const void *dy, const float *mean, const float *rstd, const int64_t *offsets, int64_t B,
+                            int64_t rows, int64_t reps, int64_t N, void *dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream) {
+    return norm_backward("jfa_layer_norm_backward", false, x, weight, dy, mean, rstd, offsets, B, rows, reps, N, dx, dweight, dbias, workspace, workspace_bytes,
+                         (hipStream_t)stream);
+}
+int jfa_layer_norm_backward_f32(const float *x, const float *weight, const float *dy, const float *mean, const float *rstd, const int64_t *offsets, int64_t B,
+                                int64_t rows, int64_t reps, int64_t N, float *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                                void *stream) {
+    return norm_backward("jfa_layer_norm_backward_f32", true, x, weight, dy, mean, rstd, offsets, B, rows, reps, N, dx, dweight, dbias, workspace,
+                         workspace_bytes, (hipStream_t)stream);
+}
+
+// ---- embedding lookup ----
+
+namespace {
+int embedding_begin(const char *who, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, int id_bytes) {
+    const int st = rows_begin(who, offsets, B, rows, N);
+    if (st != JFA_OK) return st;
+    if (V <= 0 || V > JFA_ROWS_MAX) return fail(V <= 0 ? JFA_ERR_INVALID_ARG : JFA_ERR_UNSUPPORTED, "%s: bad V = %lld", who, (long long)V);
+    if (id_bytes != 4 && id_bytes != 8) return fail(JFA_ERR_INVALID_ARG, "%s: id_bytes = %d is neither 4 nor 8", who, id_bytes);
+    return JFA_OK;
+}
+int embedding_forward(const char *who, bool f32, const void *table, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V,
+                      int64_t N, float scale, void *out, hipStream_t s) {
+    int st = embedding_begin(who, offsets, B, rows, V, N, id_bytes);
+    if (st != JFA_OK || rows == 0) return st;
+    const size_t size = f32 ? 4 : 2;
+    st = rows_pointers(who, {{"table", table, size, true}, {"ids", ids, (size_t)id_bytes, true}, {"out", out, size, true}, {"offsets", offsets, 8, false}});
+    if (st != JFA_OK) return st;
+    ScopedTimer tm("embedding", s);
+    const hipError_t e = jfa::launch_embedding(f32, table, ids, id_bytes == 8, offsets, B, rows, V, N, scale, out, s);
+    return e == hipSuccess ? JFA_OK : hip_fail("embedding kernel", e);
+}
+int embedding_backward(const char *who, bool f32, const void *dout, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V,
+                       int64_t N, float scale, void *dtable, void *workspace, size_t workspace_bytes, hipStream_t s) {
+    int st = embedding_begin(who, offsets, B, rows, V, N, id_bytes);
+    if (st != JFA_OK) return st;
+    const size_t size = f32 ? 4 : 2;
+    st = rows_pointers(who, {{"dout", dout, size, rows > 0}, {"ids", ids, (size_t)id_bytes, rows > 0}, {"dtable", dtable, size, true}, {"offsets", offsets, 8, false}});
+    if (st != JFA_OK) return st;
+    const size_t need = jfa::embedding_workspace(rows, V, N);
+    if (workspace_bytes < need || !workspace)
+        return fail(JFA_ERR_INVALID_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : 0, need);
+    if (misaligned(workspace)) return fail(JFA_ERR_INVALID_ARG, "%s: the workspace is not 16-byte aligned", who);
+    ScopedTimer tm("embedding_bwd", s);
+    const hipError_t e = jfa::launch_embedding_backward(f32, dout, ids, id_bytes == 8, offsets, B, rows, V, N, scale, dtable, workspace, s);
+    return e == hipSuccess ? JFA_OK : hip_fail("embedding backward kernel", e);
+}
+}  // namespace
+
+size_t jfa_embedding_workspace_bytes(int64_t rows, int64_t V, int64_t N) {
+    if (embedding_begin("jfa_embedding_workspace_bytes", nullptr, 0, rows, V, N, 8) != JFA_OK) return 0;
+    return jfa::embedding_workspace(rows, V, N);
+}
+int jfa_embedding(const void *table, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale,
+                  void *out, void *stream) {
+    return embedding_forward("jfa_embedding", false, table, ids, id_bytes, offsets, B, rows, V, N, scale, out, (hipStream_t)stream);
+}
+int jfa_embedding_f32(const float *table, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale,
+                      float *out, void *stream) {
+    return embedding_forward("jfa_embedding_f32", true, table, ids, id_bytes, offsets, B, rows, V, N, scale, out, (hipStream_t)stream);
+}
+int jfa_embedding_backward(const void *dout, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale,
+                           void *dtable, void *workspace, size_t workspace_bytes, void *stream) {
+    return embedding_backward("jfa_embedding_backward", false, dout, ids, id_bytes, offsets, B, rows, V, N, scale, dtable, workspace, workspace_bytes,
+                              (hipStream_t)stream);
+}
+int jfa_embedding_backward_f32(const float *dout, const void *ids, int id_bytes, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N,
+                               float scale, float *dtable, void *workspace, size_t workspace_bytes, void *stream) {
+    return embedding_backward("jfa_embedding_backward_f32", true, dout, ids, id_bytes, offsets, B, rows, V, N, scale, dtable, workspace, workspace_bytes,
+                              (hipStream_t)stream);
 }
 
 }  // extern "C"

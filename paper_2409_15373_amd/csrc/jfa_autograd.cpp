@@ -13,7 +13,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
+#include <unordered_set>
 
 namespace {
 
@@ -354,6 +356,28 @@ PyMethodDef calls[] = {JFA_CALL("forward", forward_call<false>),
                        {nullptr, nullptr, 0, nullptr}};
 #undef JFA_CALL
 
+// In a backward: whether a graph is being captured that gradients would leave.  Autograd runs a node, and what adds up a leaf's gradient, on the
+// stream that was current when it was made, and makes that stream wait for the one that the gradient comes from.  A leaf whose
+// gradient has been asked for on another stream by a graph that is still alive keeps that graph's node; captured, the wait draws the other stream
+// into the capture, which then cannot be ended (the process ends instead).
+bool gradients_leave_capture() {
+    if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return false;
+    const c10::StreamId here = c10::hip::getCurrentHIPStream().id();
+    const std::shared_ptr<torch::autograd::Node> node = torch::autograd::get_current_node();
+    if (!node) return false;
+    std::unordered_set<torch::autograd::Node *> seen{node.get()};
+    std::vector<torch::autograd::Node *> todo{node.get()};
+    while (!todo.empty()) {
+        torch::autograd::Node *const at = todo.back();
+        todo.pop_back();
+        const auto stream = at->stream();
+        if (stream && stream->id() != here) return true;
+        for (const torch::autograd::Edge &e : at->next_edges())
+            if (e.function && seen.insert(e.function.get()).second) todo.push_back(e.function.get());
+    }
+    return false;
+}
+
 // entry: name of an entry point -> its address
 void bind_library(const std::function<int64_t(const std::string &)> &entry, pybind11::object check, pybind11::object pointer) {
     const char *suffix[2] = {"", "_f32"};
@@ -383,5 +407,6 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     m.def("bind_library", &bind_library);
     m.def("self_attention", &self_attention);
     m.def("cross_attention", &cross_attention);
+    m.def("gradients_leave_capture", &gradients_leave_capture);
     if (PyModule_AddFunctions(m.ptr(), calls) != 0) throw pybind11::error_already_set();
 }

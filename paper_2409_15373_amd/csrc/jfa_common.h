@@ -820,4 +820,40 @@ hipError_t launch_jagged_jagged_bmm(const void *x, const void *y, const int64_t 
 hipError_t launch_jagged_softmax(bool backward, const void *a, const void *b, const int64_t *offsets, int B, int64_t max_len, int D,
                                  int32_t *counter, void *out, int cus, hipStream_t stream);
 
+// Linear attention with a decay for each head (jfa_linear.hip): up to three walks over the samples in one launch.
+struct LinearWalk {
+    const void *a, *b, *c;   // what the walk takes for queries, keys and values
+    void *out;
+    const float *state_in;   // [B, H, D, D], or null for zeros
+    float *state_out;        // or null
+    float in_scale, out_scale;   // on what enters the state, on what comes out of it
+    bool reverse;            // from the last row of a sample to the first; a row enters before the decay
+    bool transposed;         // state_in and state_out have the dimension of c first
+};
+struct LinearWalks { LinearWalk walk[3]; };
+constexpr int kLinearCus = 256;   // compute units: the workspace's size follows from the sizes alone
+int linear_segment_rows(int64_t B, int64_t max_len, int H, int walks, int cus);
+hipError_t launch_linear_walks(bool f32, const LinearWalks &walks, int n_walks, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
+                               int D, int segments, int segment_rows, float *carried, hipStream_t stream);
+hipError_t launch_linear_step(bool f32, const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
+                              const float *state, void *out, float *new_state, hipStream_t stream);
+
+// Whether 16-byte accesses may start at all of these (null: not there).
+template <typename... P> inline bool aligned16(const P *...p) { return (((uintptr_t)p | ...) & 15u) == 0; }
+
+// Layer norm of the rows of a jagged tensor (jfa_layer_norm.hip): `reps` rows of N elements to each of the tensor's rows.
+size_t layer_norm_workspace(int64_t rows, int64_t N);
+hipError_t launch_layer_norm(bool f32, const void *x, const void *weight, const void *bias, const int64_t *offsets, int64_t B, int64_t rows, int64_t reps,
+                             int64_t N, float eps, void *y, float *mean, float *rstd, hipStream_t stream);
+hipError_t launch_layer_norm_backward(bool f32, const void *x, const void *weight, const void *dy, const float *mean, const float *rstd, const int64_t *offsets,
+                                      int64_t B, int64_t rows, int64_t reps, int64_t N, void *dx, void *dweight, void *dbias, void *workspace,
+                                      hipStream_t stream);
+
+// Embedding lookup into a jagged tensor and its gradient (jfa_embedding.hip).
+size_t embedding_workspace(int64_t rows, int64_t V, int64_t N);
+hipError_t launch_embedding(bool f32, const void *table, const void *ids, bool ids64, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N,
+                            float scale, void *out, hipStream_t stream);
+hipError_t launch_embedding_backward(bool f32, const void *dout, const void *ids, bool ids64, const int64_t *offsets, int64_t B, int64_t rows, int64_t V,
+                                     int64_t N, float scale, void *dtable, void *workspace, hipStream_t stream);
+
 }  // namespace jfa
