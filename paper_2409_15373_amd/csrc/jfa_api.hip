@@ -825,20 +825,20 @@ int linear_pointers(const char *who, const void *const *tensors, int n, const fl
         if (misaligned(optional[i])) return fail(JFA_ERR_INVALID_ARG, "%s: a state is not 16-byte aligned", who);
     return JFA_OK;
 }
-size_t linear_workspace(int64_t B, int64_t max_len, int H, int D, int walks, int *segments, int *segment_rows) {
-    *segment_rows = jfa::linear_segment_rows(B, max_len, H, walks, jfa::kLinearCus);
+size_t linear_workspace(int64_t B, int64_t max_len, int H, int D, bool backward, int *segments, int *segment_rows) {
+    *segment_rows = jfa::linear_segment_rows(B, max_len, H, backward ? 3 : 1, jfa::kLinearCus);
     *segments = max_len > *segment_rows ? (int)((max_len + *segment_rows - 1) / *segment_rows) : 1;
-    return (size_t)(walks * B * H * (*segments - 1)) * D * D * sizeof(float);
+    return (size_t)((backward ? 2 : 1) * B * H * (*segments - 1)) * D * D * sizeof(float);
 }
-int linear_launch(const char *who, bool f32, const jfa::LinearWalks &walks, int n_walks, bool states, const float *log_decay, const int64_t *offsets,
+int linear_launch(const char *who, bool f32, const jfa::LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets,
                   int64_t B, int64_t max_len, int H, int D, void *workspace, size_t workspace_bytes, hipStream_t s) {
     int segments, segment_rows;
-    const size_t need = linear_workspace(B, max_len, H, D, n_walks, &segments, &segment_rows);
+    const size_t need = linear_workspace(B, max_len, H, D, backward, &segments, &segment_rows);
     if (workspace_bytes < need || (need && !workspace))
         return fail(JFA_ERR_INVALID_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : 0, need);
     if (need && misaligned(workspace)) return fail(JFA_ERR_INVALID_ARG, "%s: the workspace is not 16-byte aligned", who);
-    ScopedTimer tm(n_walks == 1 ? "linear_attention" : "linear_attention_bwd", s);
-    const hipError_t e = jfa::launch_linear_walks(f32, walks, n_walks, states, log_decay, offsets, B, H, D, segments, segment_rows, (float *)workspace, s);
+    ScopedTimer tm(backward ? "linear_attention_bwd" : "linear_attention", s);
+    const hipError_t e = jfa::launch_linear_walks(f32, walks, backward, states, log_decay, offsets, B, H, D, segments, segment_rows, (float *)workspace, s);
     return e == hipSuccess ? JFA_OK : hip_fail("linear attention kernel", e);
 }
 int linear_forward(const char *who, bool f32, const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B,
@@ -849,8 +849,8 @@ int linear_forward(const char *who, bool f32, const void *q, const void *k, cons
     const void *tensors[] = {q, k, v, out, offsets, log_decay};
     const float *states[] = {initial_state, final_state};
     if ((st = linear_pointers(who, tensors, 6, states, 2)) != JFA_OK) return st;
-    const jfa::LinearWalks walks{{{q, k, v, out, initial_state, final_state, 1.0f, scale, false, false}}};
-    return linear_launch(who, f32, walks, 1, final_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
+    const jfa::LinearWalks walks{{{q, k, v, out, initial_state, final_state, 1.0f, scale, false, false, false, 0}}};
+    return linear_launch(who, f32, walks, false, final_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
 }
 int linear_backward(const char *who, bool f32, const void *q, const void *k, const void *v, const void *dout, const float *log_decay,
                     const int64_t *offsets, int64_t B, int64_t max_len, int H, int D, float scale, const float *initial_state,
@@ -861,10 +861,10 @@ int linear_backward(const char *who, bool f32, const void *q, const void *k, con
     const void *tensors[] = {q, k, v, dout, dq, dk, dv, offsets, log_decay};
     const float *states[] = {initial_state, dfinal_state, dinitial_state};
     if ((st = linear_pointers(who, tensors, 9, states, 3)) != JFA_OK) return st;
-    const jfa::LinearWalks walks{{{dout, v, k, dq, initial_state, nullptr, 1.0f, scale, false, true},
-                                  {v, dout, q, dk, dfinal_state, nullptr, scale, 1.0f, true, true},
-                                  {k, q, dout, dv, dfinal_state, dinitial_state, scale, 1.0f, true, false}}};
-    return linear_launch(who, f32, walks, 3, dinitial_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
+    const jfa::LinearWalks walks{{{dout, v, k, dq, initial_state, nullptr, 1.0f, scale, false, true, false, 0},
+                                  {v, dout, q, dk, dfinal_state, nullptr, scale, 1.0f, true, true, true, 1},   // the two have one state
+                                  {k, q, dout, dv, dfinal_state, dinitial_state, scale, 1.0f, true, false, false, 1}}};
+    return linear_launch(who, f32, walks, true, dinitial_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
 }
 int linear_step(const char *who, bool f32, const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
                 const float *state, void *out, float *new_state, hipStream_t s) {
@@ -881,7 +881,7 @@ int linear_step(const char *who, bool f32, const void *q, const void *k, const v
 size_t jfa_linear_attention_workspace_bytes(int64_t B, int64_t max_len, int H, int D, int pass) {
     if (linear_begin("jfa_linear_attention_workspace_bytes", B, max_len, H, D) != JFA_OK || B == 0) return 0;
     int segments, segment_rows;
-    return linear_workspace(B, max_len, H, D, pass ? 3 : 1, &segments, &segment_rows);
+    return linear_workspace(B, max_len, H, D, pass != 0, &segments, &segment_rows);
 }
 int jfa_linear_attention(const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len, int H,
                          int D, float scale, const float *initial_state, void *out, float *final_state, void *workspace, size_t workspace_bytes,

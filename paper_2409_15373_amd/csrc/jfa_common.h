@@ -829,11 +829,13 @@ struct LinearWalk {
     float in_scale, out_scale;   // on what enters the state, on what comes out of it
     bool reverse;            // from the last row of a sample to the first; a row enters before the decay
     bool transposed;         // state_in and state_out have the dimension of c first
+    bool carried_transposed; // so do the states between segments
+    int carried;             // which of those between segments are this walk's
 };
 struct LinearWalks { LinearWalk walk[3]; };
 constexpr int kLinearCus = 256;   // compute units: the workspace's size follows from the sizes alone
 int linear_segment_rows(int64_t B, int64_t max_len, int H, int walks, int cus);
-hipError_t launch_linear_walks(bool f32, const LinearWalks &walks, int n_walks, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
+hipError_t launch_linear_walks(bool f32, const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
                                int D, int segments, int segment_rows, float *carried, hipStream_t stream);
 hipError_t launch_linear_step(bool f32, const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
                               const float *state, void *out, float *new_state, hipStream_t stream);

@@ -12,6 +12,7 @@
 //
 // Each row of a tensor is read once and each output row written once: at 96 flops a byte (D = 128, 64 rows) that is bound by HBM.
 #include "jfa_common.h"
+#include "jfa_lds.h"
 #include "jfa_mfma.h"
 
 namespace jfa {
@@ -19,27 +20,36 @@ namespace jfa {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) float f32x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
-// The two element types.  An operand holds 16 contraction indices, eight per lane: slot e of a lane in half h = lane / 32 is index
-// (e / 4) * 8 + 4 h + e % 4, the order in which an accumulator tile holds its rows, so that a tile is an operand as it stands.
-// rows(): the tile's rows along the lanes, contraction along its columns; cols(): its columns along the lanes, contraction along its rows.
+// A tile in LDS: kRows rows without padding, in 16-byte chunks, as the copies from memory leave them.  The chunks of a row are in another order in every
+// row, chunk c at place c ^ swizzle(row), so that neither 16 rows' same chunk nor four consecutive rows' same 64 bytes meet in a bank.
+template <int kChunks> __host__ __device__ constexpr int swizzle(int row) {
+    return kChunks >= 16 ? ((row & 3) << 2) | ((row >> 2) & 3) : kChunks == 8 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : (row >> 2) & 3;
+}
+
+// The two element types.  An operand holds 16 contraction indices, eight per lane.
+// rows(): the tile's rows along the lanes, contraction along its columns, slot e of a lane in half h = lane / 32 column 8 h + e of 16.
+// cols(): its columns along the lanes, contraction along its rows, slot e row (e / 4) * 8 + 4 h + e % 4 of 16: the order in which an accumulator tile
+// holds its rows, so that a tile of products of rows (P) is an operand as it stands.  PERMUTED: lane l has column l with bits 2 and 3 exchanged: what is
+// accumulated over such a column (the state) is, as it stands, an operand in the order of rows().
+__device__ inline int exchanged(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
 template <typename T> struct Elem;
 
 template <> struct Elem<__bf16> {
     typedef bf16x8 Operand;
-    static constexpr int kRows = 64;
-    __host__ __device__ static constexpr int row_bytes(int d) { return d * 2 + 32; }
+    static constexpr int kRows = 64, kSplit = 2;
     __device__ static f32x16 product(Operand a, Operand b, f32x16 c) { return mfma_32x32x16(a, b, c); }
-    __device__ static Operand rows(const char *tile, int stride, int row0, int k0, int lane) {
-        const char *p = tile + (row0 + (lane & 31)) * stride + (k0 + 4 * (lane >> 5)) * 2;
-        const u32x2 lo = *reinterpret_cast<const u32x2 *>(p), hi = *reinterpret_cast<const u32x2 *>(p + 16);
-        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+    // what a lane adds to (or exchanges bits of) every address
+    template <int D> __device__ static int rows_base(int lane) { return (lane & 31) * D * 2 + ((swizzle<D / 8>(lane & 31) ^ (lane >> 5)) << 4); }
+    template <int D, bool PERMUTED> __device__ static int cols_base(int lane) {
+        const int half = lane >> 5, row = 4 * half + ((lane & 15) >> 2), q = PERMUTED ? ((lane & 1) << 1) | ((lane >> 1) & 1) : lane & 3;
+        return row * D * 2 + (((((lane >> 4) & 1) * 2 + (q >> 1)) ^ swizzle<D / 8>(row)) << 4) + (q & 1) * 8;
     }
-    __device__ static Operand cols(const char *tile, int stride, int col0, int k0, int lane) {
-        const char *p = tile + (k0 + 4 * (lane >> 5) + ((lane & 15) >> 2)) * stride + col0 * 2 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-        return concat(lds_read_tr16(p), lds_read_tr16(p + 8 * stride));
+    template <int D> __device__ static Operand rows(const char *tile, int base, int row0, int k0) { return lds_read_b128(tile + row0 * D * 2 + (base ^ (k0 * 2))); }
+    template <int D> __device__ static Operand cols(const char *tile, int base, int col0, int k0) {
+        const char *const p = tile + k0 * D * 2;
+        const int at = base ^ (col0 * 2);
+        return concat(lds_read_tr16(p + at), lds_read_tr16(p + 8 * D * 2 + (at ^ 32)));
     }
     __device__ static Operand pack(const f32x8 &x) {
         Operand r;
@@ -63,23 +73,29 @@ template <> struct Elem<__bf16> {
 
 template <> struct Elem<float> {
     typedef f32x8 Operand;
-    static constexpr int kRows = 32;
-    __host__ __device__ static constexpr int row_bytes(int d) { return d * 4 + 16; }
+    static constexpr int kRows = 32, kSplit = 1;
     __device__ static f32x16 product(Operand a, Operand b, f32x16 c) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
         return c;
     }
-    __device__ static Operand rows(const char *tile, int stride, int row0, int k0, int lane) {
-        const char *p = tile + (row0 + (lane & 31)) * stride + (k0 + 4 * (lane >> 5)) * 4;
-        const f32x4 lo = *reinterpret_cast<const f32x4 *>(p), hi = *reinterpret_cast<const f32x4 *>(p + 32);
+    template <int D> __device__ static int rows_base(int lane) { return (lane & 31) * D * 4 + ((swizzle<D / 4>(lane & 31) ^ ((lane >> 5) * 2)) << 4); }
+    template <int D, bool PERMUTED> __device__ static int cols_base(int lane) {
+        const int half = lane >> 5, col = PERMUTED ? exchanged(lane & 31) : lane & 31;
+        return 4 * half * D * 4 + (((col >> 2) ^ swizzle<D / 4>(4 * half)) << 4) + (col & 3) * 4;
+    }
+    template <int D> __device__ static Operand rows(const char *tile, int base, int row0, int k0) {
+        const char *const p = tile + row0 * D * 4;
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(p + (base ^ (k0 * 4))), hi = *reinterpret_cast<const f32x4 *>(p + (base ^ (k0 * 4 + 16)));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    __device__ static Operand cols(const char *tile, int stride, int col0, int k0, int lane) {
-        const char *p = tile + (k0 + 4 * (lane >> 5)) * stride + (col0 + (lane & 31)) * 4;
+    template <int D> __device__ static Operand cols(const char *tile, int base, int col0, int k0) {
         Operand r;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = *reinterpret_cast<const float *>(p + ((e >> 2) * 8 + (e & 3)) * stride);
+        for (int e = 0; e < 8; ++e) {
+            const int row = (e >> 2) * 8 + (e & 3);
+            r[e] = *reinterpret_cast<const float *>(tile + (k0 + row) * D * 4 + (base ^ (col0 * 4) ^ (swizzle<D / 4>(row) << 4)));
+        }
         return r;
     }
     __device__ static Operand pack(const f32x8 &x) { return x; }
@@ -99,25 +115,40 @@ __device__ inline float log2_decay(float log_decay) {
     const float x = log_decay * 1.4426950408889634f;
     return x < -1024.0f ? -1024.0f : x;
 }
+// s_waitcnt for vector memory alone: at most `left` pending (the fields of the other counters at their maximum)
+template <int left> constexpr int vmem_left() { return (left & 15) | ((left >> 4) << 14) | (7 << 4) | (15 << 8); }
+constexpr int kNoVmem = vmem_left<0>();
 __device__ inline float power(float log2_g, int n) { return fast_exp2(log2_g * (float)n); }   // n >= 0
 
 }  // namespace
 
-// One walk per blockIdx.y, one (sample, head, segment) per blockIdx.x; D / 32 waves.  Wave w owns columns 32 w .. 32 w + 31 of the state and of
-// the outputs.  kParts: into how many bf16 parts the decayed rows of C are split for the state's product: one where the state only
-// feeds bf16 outputs, three (exact) where it is itself a result.
+// A workgroup takes one (sample, head, segment), blockIdx.x, through ROLES walks that go the same way over the same tensors: one of them (walk
+// blockIdx.y), or the two that give dk and dv, which share the tiles of q and dout.  Each walk has D / 32 waves; wave w of it owns columns
+// 32 w .. 32 w + 31 of the state and of the outputs.
+// bf16: what is rounded in front of a product (P, the state as a factor of out, the decayed rows of C) is split into two bf16 numbers, 16 bits in
+// all, so that a result's error is its own rounding (one bf16 number each: 1.65 times that, root mean square); kParts = 3, exact, for the decayed
+// rows where the state is itself a result.  The matrix instructions have the time: they are busy a third of a chunk's way through memory.
 // kStateOnly: the state that a segment adds to, for those with a segment after them, into `carried`.
-template <typename T, int D, int kParts, bool kStateOnly>
-__global__ __launch_bounds__(2 * D) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
-                                                            int H, int segments, int segment_rows, float *__restrict__ carried) {
+template <typename T, int D, int ROLES, int kParts, bool kStateOnly>
+__global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
+                                                                       int H, int segments, int segment_rows, float *__restrict__ carried) {
     typedef Elem<T> E;
     typedef typename E::Operand Operand;
-    constexpr int kRows = E::kRows, kThreads = 2 * D, kRowBytes = E::row_bytes(D), kSize = (int)sizeof(T);
-    constexpr int kTiles = kRows / 32, kStateTiles = D / 32, kSteps = D / 16;
-    constexpr int kPRow = kRows * kSize + 16;
-    constexpr int kChunksPerRow = D * kSize / 16, kLoads = kRows * kChunksPerRow / kThreads;   // 16-byte chunks of a tile per thread
-    __shared__ __attribute__((aligned(16))) char at[kStateOnly ? 16 : kRows * kRowBytes], bt[kRows * kRowBytes], ct[kRows * kRowBytes], pt[kStateOnly ? 16 : kRows * kPRow];
-    const LinearWalk &walk = walks.walk[blockIdx.y];
+    constexpr int kRows = E::kRows, kSize = (int)sizeof(T), kStateTiles = D / 32, kSteps = D / 16, kSplit = E::kSplit, kWaves = kStateTiles * ROLES;
+    constexpr int kTiles = kRows / 32, kPTiles = kTiles * (kTiles + 1) / 2;
+    constexpr int kChunks = D * kSize / 16, kTileBytes = kRows * kChunks * 16, kLoads = kRows * kChunks / (64 * kWaves);   // 16-byte chunks of a row; copies of a tile per wave
+    // Places of tiles.  Two walks: two of each tile, the next chunk's are on their way while this one's are in use.  One walk: two workgroups of a
+    // compute unit have room for four tiles each: A, C and two of B; the next B is fetched from the start of a chunk on, the next A once the state's
+    // product with A is done, the next C once the chunk is, which is in time for the products with C of the next chunk.
+    constexpr int kPlaces = ROLES == 2 ? 8 : 4;
+    __shared__ __attribute__((aligned(16))) char lds[kPlaces * kTileBytes];
+    __shared__ float powers[ROLES][2][2 * kRows];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int role = ROLES == 2 ? wave / kStateTiles : 0, strip = ROLES == 2 ? wave % kStateTiles : wave;
+    const int col = lane & 31, half = lane >> 5;
+    const int which = ROLES == 2 ? 1 : (int)blockIdx.y;   // the first role's walk
+    const LinearWalk &walk = walks.walk[which + role];
     const int pair = blockIdx.x / segments, segment = blockIdx.x - pair * segments;
     const int b = pair / H, h = pair - b * H;
     const int64_t first = offsets[b];
@@ -127,165 +158,247 @@ __global__ __launch_bounds__(2 * D) void linear_walk_kernel(LinearWalks walks, c
     if (kStateOnly ? last || segment == segments - 1 : (t0 >= L && segment > 0)) return;
     const int64_t left = L - t0;
     const int n = (int)(left < segment_rows ? left : segment_rows);   // rows of this segment; 0 for an empty sample
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 31, half = lane >> 5;
     const bool reverse = walk.reverse;
     const float lg = log2_decay(log_decay[h]);
-    float *const state_out = kStateOnly ? carried + (((int64_t)blockIdx.y * (gridDim.x / segments) + pair) * (segments - 1) + segment) * D * D
-                                        : last && walk.state_out ? walk.state_out + (int64_t)pair * D * D : nullptr;
-    const bool out_transposed = !kStateOnly && walk.transposed;
+    float *const passed = carried + ((int64_t)walk.carried * (gridDim.x / segments) + pair) * (segments - 1) * D * D;
+    float *const state_out = kStateOnly ? passed + (int64_t)segment * D * D : last && walk.state_out ? walk.state_out + (int64_t)pair * D * D : nullptr;
 
-    f32x16 S[kStateTiles];   // tile m: rows 32 m .. (dimension of B), columns 32 wave .. (dimension of C)
+    f32x16 S[kStateTiles];   // tile m: rows 32 m .. (dimension of B), columns 32 strip .. (dimension of C)
 #pragma unroll
     for (int m = 0; m < kStateTiles; ++m)
 #pragma unroll
         for (int v = 0; v < 16; ++v) S[m][v] = 0.0f;
     if (!kStateOnly) {
-        const float *from = segment > 0 ? carried + (((int64_t)blockIdx.y * (gridDim.x / segments) + pair) * (segments - 1) + segment - 1) * D * D
-                            : walk.state_in ? walk.state_in + (int64_t)pair * D * D : nullptr;
+        const float *from = segment > 0 ? passed + (int64_t)(segment - 1) * D * D : walk.state_in ? walk.state_in + (int64_t)pair * D * D : nullptr;
         if (from) {
-            const bool transposed = segment == 0 && walk.transposed;
+            const bool transposed = segment == 0 ? walk.transposed : walk.carried_transposed;
 #pragma unroll
             for (int m = 0; m < kStateTiles; ++m)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const int r = m * 32 + acc_row(v, half), c = wave * 32 + col;
+                    const int r = m * 32 + exchanged(acc_row(v, half)), c = strip * 32 + col;
                     S[m][v] = from[transposed ? c * D + r : r * D + c];
                 }
         }
     }
 
-    // Row t of the walk is row first + t, or first + L - 1 - t, of the tensors.
-    const int64_t row_stride = (int64_t)H * D, step = reverse ? -row_stride : row_stride;
-    const int64_t base = (first + (reverse ? L - 1 - t0 : t0)) * row_stride + (int64_t)h * D;
-    const T *const sources[3] = {(const T *)walk.a + base, (const T *)walk.b + base, (const T *)walk.c + base};
-    u32x4 held[3][kLoads];
-    auto fetch = [&](int r0) {
+    // Row t of the walk is row first + t, or first + L - 1 - t, of the tensors.  A chunk's rows are kRows rows from `low` on (where it is
+    // the last and walked backwards, its first ones lie in front of the sample and are not touched): 32-bit offsets from there.
+    const uint32_t row_bytes = (uint32_t)H * D * kSize;
+    int64_t low = ((first + (reverse ? L - t0 - kRows : t0)) * H + h) * D;
+    const int64_t low_step = (reverse ? -(int64_t)kRows : (int64_t)kRows) * H * D;
+    const T *const a0 = (const T *)walks.walk[which].a, *const a1 = (const T *)walks.walk[ROLES == 2 ? 2 : which].a;
+    const T *const b0 = (const T *)walks.walk[which].b, *const c0 = (const T *)walks.walk[which].c;
+    // The rows from `rows` on are not there: the last one takes their place.  Whatever it is, P's mask and the decayed rows' zeros keep it out.
+    auto copy = [&](const T *tensor, int64_t from, int rows, int place) {
+        const T *const base = reinterpret_cast<const T *>(uniform64((int64_t)(tensor + from)));
 #pragma unroll
-        for (int s = kStateOnly ? 1 : 0; s < 3; ++s)
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const int c = tid + kThreads * u, r = r0 + c / kChunksPerRow;
-                held[s][u] = u32x4{0, 0, 0, 0};   // rows past the sample's end
-                if (r < n) held[s][u] = *reinterpret_cast<const u32x4 *>(sources[s] + r * step + (c % kChunksPerRow) * (16 / kSize));
-            }
+        for (int u = 0; u < kLoads; ++u) {
+            const int at = (u * kWaves + wave) * 64 + lane, t = at / kChunks, c = at % kChunks ^ swizzle<kChunks>(t), there = t < rows ? t : rows - 1;
+            bd_dma16(base, (uint32_t)(reverse ? kRows - 1 - there : there) * row_bytes + c * 16, lds + place * kTileBytes + (u * kWaves + wave) * 1024);
+        }
     };
+    const int row_base = E::template rows_base<D>(lane), col_base = E::template cols_base<D, false>(lane) ^ (strip * 32 * kSize), col_base_b = E::template cols_base<D, true>(lane);
 
-    // Powers of the decay.  diag: P's factors in a tile on the diagonal (column i = this lane, rows j); below it g^(32 + i - j) = g^(i + 1) g^(31 - j).
-    const float in_scale = walk.in_scale, out_scale = walk.out_scale;
-    float diag[16], below[kTiles > 1 ? 16 : 1], late[8];
-    if (!kStateOnly) {
+    // powers[0][kRows + x]: in_scale g^x, zero for negative x: P's factors.  powers[1]: with the decay after a chunk's last row, `tail`: the state's.
+    const int tail = reverse ? 1 : 0;
+    float (*const my_powers)[2 * kRows] = powers[role];
+    for (int i = strip * 64 + lane; i < 2 * 2 * kRows; i += 64 * kStateTiles) {
+        const int x = i % (2 * kRows) - kRows;
+        my_powers[i / (2 * kRows)][x + kRows] = x < 0 ? 0.0f : walk.in_scale * power(lg, x + (i < 2 * kRows ? 0 : tail));
+    }
+    const float out_scale = walk.out_scale;
+    float since[kTiles];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int j = acc_row(v, half);
-            diag[v] = col >= j ? in_scale * power(lg, col - j) : 0.0f;
-            if (kTiles > 1) below[v] = in_scale * power(lg, 31 - j + col + 1);
+    for (int ti = 0; ti < kTiles; ++ti) since[ti] = power(lg, ti * 32 + col + 1 - tail);
+
+    if (n > 0) {
+        if constexpr (ROLES == 2) {
+            copy(a0, low, n, 0);
+            copy(a1, low, n, 1);
+            copy(b0, low, n, 2);
+            copy(c0, low, n, 3);
+        } else {
+            copy(b0, low, n, 2);
+            if (!kStateOnly) copy(a0, low, n, 0);
         }
     }
-    // late[e]: g^(15 - index) of a contraction step's rows; times g^(16 (steps left)) it is a row's decay up to the chunk's end
-#pragma unroll
-    for (int e = 0; e < 8; ++e) late[e] = in_scale * power(lg, 15 - ((e >> 2) * 8 + 4 * half + (e & 3)));
-    const float chunk_decay = power(lg, kRows);
-    const int tail = reverse ? 1 : 0;   // the decay after a chunk's last row
-
-    fetch(0);
-    for (int r0 = 0; r0 < n; r0 += kRows) {
+    for (int r0 = 0, turn = 0; r0 < n; r0 += kRows, low += low_step, turn ^= 1) {
         const int rows = n - r0 < kRows ? n - r0 : kRows;
-        __syncthreads();   // the previous chunk's tiles are free
-#pragma unroll
-        for (int s = kStateOnly ? 1 : 0; s < 3; ++s) {
-            char *tile = s == 0 ? at : s == 1 ? bt : ct;
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const int c = tid + kThreads * u;
-                *reinterpret_cast<u32x4 *>(tile + (c / kChunksPerRow) * kRowBytes + (c % kChunksPerRow) * 16) = held[s][u];
+        const bool more = r0 + kRows < n;
+        __builtin_amdgcn_s_waitcnt(kNoVmem);
+        __syncthreads();   // the tiles fetched so far are there, and the last chunk's are free
+        if constexpr (ROLES == 2) {
+            if (more) {
+                copy(a0, low + low_step, n - r0 - kRows, 4 * (turn ^ 1));
+                copy(a1, low + low_step, n - r0 - kRows, 4 * (turn ^ 1) + 1);
+                copy(b0, low + low_step, n - r0 - kRows, 4 * (turn ^ 1) + 2);
+                copy(c0, low + low_step, n - r0 - kRows, 4 * (turn ^ 1) + 3);
             }
+        } else {
+            copy(c0, low, n - r0, 1);
+            if (more) copy(b0, low + low_step, n - r0 - kRows, 2 + (turn ^ 1));
         }
-        __syncthreads();
-        if (r0 + kRows < n) fetch(r0 + kRows);
+        // (C waits for its copies, at most the next B's later: stores have been waited for above)
+        auto c_is_there = [&]() {
+            if constexpr (ROLES == 1) {
+                if (more) __builtin_amdgcn_s_waitcnt(vmem_left<kLoads>());
+                else __builtin_amdgcn_s_waitcnt(kNoVmem);
+                __syncthreads();
+            }
+        };
+        const char *const at = lds + (ROLES == 2 ? 4 * turn + role : 0) * kTileBytes;
+        const char *const bt = lds + (ROLES == 2 ? 4 * turn + 2 + role : 2 + turn) * kTileBytes, *const ct = lds + (ROLES == 2 ? 4 * turn + 3 - role : 1) * kTileBytes;
+        Operand c[2 * kTiles];   // the chunk's rows of C, this wave's columns
+        if (kStateOnly) {
+            c_is_there();
+#pragma unroll
+            for (int k = 0; k < 2 * kTiles; ++k) c[k] = E::template cols<D>(ct, col_base, 0, k * 16);
+        }
         if (!kStateOnly) {
-            // P^T, tile (rows j of B) x (columns i of A) by tile; it is zero above the diagonal
-            int t = 0;
+            // P^T, tiles (rows j of B) x (columns i of A), zero above the diagonal: every wave has all of it, as operands
+            Operand P[kPTiles][2][kSplit];
+            {
+                f32x16 p[kPTiles];
+#pragma unroll
+                for (int t = 0; t < kPTiles; ++t)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) p[t][v] = 0.0f;
+                // operands one step ahead of the products that use them: left alone, every read sits right in front of its product
+                Operand a[2][kTiles], x[2][kTiles];
+                auto read = [&](int ks) {
+#pragma unroll
+                    for (int ti = 0; ti < kTiles; ++ti) {
+                        a[ks & 1][ti] = E::template rows<D>(at, row_base, ti * 32, ks * 16);
+                        x[ks & 1][ti] = E::template rows<D>(bt, row_base, ti * 32, ks * 16);
+                    }
+                };
+                read(0);
+#pragma unroll
+                for (int ks = 0; ks < kSteps; ++ks) {
+                    if (ks + 1 < kSteps) read(ks + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    p[0] = E::product(x[ks & 1][0], a[ks & 1][0], p[0]);
+                    if constexpr (kTiles == 2) {
+                        p[1] = E::product(x[ks & 1][0], a[ks & 1][1], p[1]);
+                        p[2] = E::product(x[ks & 1][1], a[ks & 1][1], p[2]);
+                    }
+                }
+                const float *const near = my_powers[0] + kRows + col - 4 * half;   // [-(8 g + e)]: g^(i - j)
+#pragma unroll
+                for (int t = 0; t < kPTiles; ++t) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float weight = near[(t == 1 ? 32 : 0) - ((v >> 2) * 8 + (v & 3))];
+                        p[t][v] = t != 1 && col < acc_row(v, half) ? 0.0f : p[t][v] * weight;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        f32x8 x = eight(p[t], k * 8);
+#pragma unroll
+                        for (int part = 0; part < kSplit; ++part) {
+                            P[t][k][part] = E::pack(x);
+                            if (part + 1 < kSplit) x -= E::widen(P[t][k][part]);
+                        }
+                    }
+                }
+            }
+            asm volatile("" ::: "memory");   // A's operands are read again: kept from above they would cost 64 registers
+            // out^T = C^T P^T + g^(i + 1) S^T A^T, this wave's columns of C
+            f32x16 o[kTiles];
 #pragma unroll
             for (int ti = 0; ti < kTiles; ++ti)
 #pragma unroll
-                for (int tj = 0; tj <= ti; ++tj, ++t) {
-                    if (t % kStateTiles != wave) continue;
-                    f32x16 p;
+                for (int v = 0; v < 16; ++v) o[ti][v] = 0.0f;
+            Operand a[2][kTiles];
+            auto read = [&](int ks) {
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) p[v] = 0.0f;
+                for (int ti = 0; ti < kTiles; ++ti) a[ks & 1][ti] = E::template rows<D>(at, row_base, ti * 32, ks * 16);
+            };
+            read(0);
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks)
-                        p = E::product(E::rows(bt, kRowBytes, tj * 32, ks * 16, lane), E::rows(at, kRowBytes, ti * 32, ks * 16, lane), p);
+            for (int ks = 0; ks < kSteps; ++ks) {
+                if (ks + 1 < kSteps) read(ks + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                f32x8 x = eight(S[ks >> 1], (ks & 1) * 8);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) p[v] = ti > tj ? p[v] * below[kTiles > 1 ? v : 0] : col < acc_row(v, half) ? 0.0f : p[v] * diag[v];
+                for (int part = 0; part < kSplit; ++part) {
+                    const Operand y = E::pack(x);
 #pragma unroll
-                    for (int g = 0; g < 4; ++g)
-                        E::store4(reinterpret_cast<T *>(pt + (ti * 32 + col) * kPRow) + tj * 32 + g * 8 + half * 4, f32x4{p[4 * g], p[4 * g + 1], p[4 * g + 2], p[4 * g + 3]});
+                    for (int ti = 0; ti < kTiles; ++ti) o[ti] = E::product(y, a[ks & 1][ti], o[ti]);
+                    if (part + 1 < kSplit) x -= E::widen(y);
                 }
-            __syncthreads();
-            // out^T = C^T P^T + g^(i + 1) S^T A^T, this wave's columns of C
+            }
+            c_is_there();   // and A is free
+            if (ROLES == 1 && more) copy(a0, low + low_step, n - r0 - kRows, 0);
+#pragma unroll
+            for (int k = 0; k < 2 * kTiles; ++k) c[k] = E::template cols<D>(ct, col_base, 0, k * 16);
+#pragma unroll
+            for (int ti = 0; ti < kTiles; ++ti)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[ti][v] *= since[ti];
+#pragma unroll
+            for (int ks = 0; ks < 2 * kTiles; ++ks)
+#pragma unroll
+                for (int part = 0; part < kSplit; ++part) {
+                    if (ks < 2) o[0] = E::product(c[ks], P[0][ks & 1][part], o[0]);
+                    if constexpr (kTiles == 2) o[1] = E::product(c[ks], P[ks < 2 ? 1 : 2][ks & 1][part], o[1]);
+                }
+            char *const out = reinterpret_cast<char *>((T *)walk.out + low);
 #pragma unroll
             for (int ti = 0; ti < kTiles; ++ti) {
-                f32x16 o;
-#pragma unroll
-                for (int v = 0; v < 16; ++v) o[v] = 0.0f;
-#pragma unroll
-                for (int ks = 0; ks < kSteps; ++ks)
-                    o = E::product(E::pack(eight(S[ks >> 1], (ks & 1) * 8)), E::rows(at, kRowBytes, ti * 32, ks * 16, lane), o);
-                const float since = power(lg, ti * 32 + col + 1 - tail);
-#pragma unroll
-                for (int v = 0; v < 16; ++v) o[v] *= since;
-#pragma unroll
-                for (int ks = 0; ks < 2 * (ti + 1); ++ks)
-                    o = E::product(E::cols(ct, kRowBytes, wave * 32, ks * 16, lane), E::rows(pt, kPRow, ti * 32, ks * 16, lane), o);
                 const int r = ti * 32 + col;
                 if (r < rows) {
-                    T *dst = (T *)walk.out + base + (r0 + r) * step + wave * 32 + half * 4;
+                    char *const dst = out + ((uint32_t)(reverse ? kRows - 1 - r : r) * row_bytes + (uint32_t)(strip * 32 + half * 4) * kSize);
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
-                        E::store4(dst + g * 8, f32x4{o[4 * g] * out_scale, o[4 * g + 1] * out_scale, o[4 * g + 2] * out_scale, o[4 * g + 3] * out_scale});
+                        E::store4(reinterpret_cast<T *>(dst + g * 8 * kSize),
+                                  f32x4{o[ti][4 * g] * out_scale, o[ti][4 * g + 1] * out_scale, o[ti][4 * g + 2] * out_scale, o[ti][4 * g + 3] * out_scale});
                 }
             }
         }
         // S <- g^rows S + (g^(rows - 1 - i) B)^T C, unless nobody looks at it any more
         if (r0 + kRows < n || state_out) {
-            const float decay = rows == kRows ? chunk_decay : power(lg, rows);
+            const float decay = power(lg, rows);
 #pragma unroll
             for (int m = 0; m < kStateTiles; ++m)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) S[m][v] *= decay;
+            const float *const left = my_powers[1] + rows - 1 - 4 * half;   // of the chunk's row i: [kRows - i]; rows that are not there have zero
+            Operand x[2][kStateTiles];
+            float weight[2][8];
+            auto read = [&](int ks) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) weight[ks & 1][e] = left[kRows - (ks * 16 + (e >> 2) * 8 + (e & 3))];
+#pragma unroll
+                for (int m = 0; m < kStateTiles; ++m) x[ks & 1][m] = E::template cols<D>(bt, col_base_b, m * 32, ks * 16);
+            };
+            read(0);
 #pragma unroll
             for (int ks = 0; ks < kRows / 16; ++ks) {
-                f32x8 c = E::widen(E::cols(ct, kRowBytes, wave * 32, ks * 16, lane));
-                if (rows == kRows) {
-                    const float rest = power(lg, kRows - 16 - ks * 16 + tail);
+                if (ks + 1 < kRows / 16) read(ks + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                f32x8 y = E::widen(c[ks]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) c[e] *= late[e] * rest;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int after = rows - 1 - (ks * 16 + (e >> 2) * 8 + 4 * half + (e & 3));
-                        c[e] *= after < 0 ? 0.0f : in_scale * power(lg, after + tail);
-                    }
-                }
+                for (int e = 0; e < 8; ++e) y[e] *= weight[ks & 1][e];
 #pragma unroll
                 for (int part = 0; part < kParts; ++part) {
-                    const Operand x = E::pack(c);
+                    const Operand z = E::pack(y);
 #pragma unroll
-                    for (int m = 0; m < kStateTiles; ++m) S[m] = E::product(E::cols(bt, kRowBytes, m * 32, ks * 16, lane), x, S[m]);
-                    if (part + 1 < kParts) c -= E::widen(x);
+                    for (int m = 0; m < kStateTiles; ++m) S[m] = E::product(x[ks & 1][m], z, S[m]);
+                    if (part + 1 < kParts) y -= E::widen(z);
                 }
             }
         }
     }
     if (state_out) {
+        const bool transposed = !kStateOnly && walk.transposed;
 #pragma unroll
         for (int m = 0; m < kStateTiles; ++m)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int r = m * 32 + acc_row(v, half), c = wave * 32 + col;
-                state_out[out_transposed ? c * D + r : r * D + c] = S[m][v];
+                const int r = m * 32 + exchanged(acc_row(v, half)), c = strip * 32 + col;
+                state_out[transposed ? c * D + r : r * D + c] = S[m][v];
             }
     }
 }
@@ -309,7 +422,7 @@ __global__ __launch_bounds__(256) void linear_carry_kernel(LinearWalks walks, co
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[e] = from[walk.transposed ? (c + e) * D + r : at + e];
     }
-    f32x4 *x = reinterpret_cast<f32x4 *>(carried + ((int64_t)blockIdx.y * (gridDim.x / blocks) + pair) * (segments - 1) * D * D + at);
+    f32x4 *x = reinterpret_cast<f32x4 *>(carried + ((int64_t)walk.carried * (gridDim.x / blocks) + pair) * (segments - 1) * D * D + at);
     const int64_t stride = (int64_t)D * D / 4;
     constexpr int kAhead = 8;
     for (int m0 = 0; m0 < n; m0 += kAhead) {
@@ -368,37 +481,45 @@ int linear_segment_rows(int64_t B, int64_t max_len, int H, int walks, int cus) {
     return (int)(rows > 0 ? rows : 64);
 }
 
-template <typename T, int D>
-static hipError_t launch_walks(const LinearWalks &walks, int n_walks, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
-                               int segments, int segment_rows, float *carried, hipStream_t stream) {
-    const dim3 grid((unsigned)(B * H * segments), n_walks), threads(2 * D);
-    constexpr int kExact = sizeof(T) == 2 ? 3 : 1;
-    if (segments > 1) {
-        if (states) hipLaunchKernelGGL((linear_walk_kernel<T, D, kExact, true>), grid, threads, 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
-        else hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, true>), grid, threads, 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
-        hipLaunchKernelGGL(linear_carry_kernel, dim3((unsigned)(B * H * (D * D / 1024)), n_walks), dim3(256), 0, stream, walks, log_decay, offsets, H, D, segments,
-                           segment_rows, carried);
+template <typename T, int D, int kParts>
+static void launch_walks(const LinearWalks &walks, bool backward, const float *log_decay, const int64_t *offsets, int64_t B, int H, int segments, int segment_rows,
+                         float *carried, hipStream_t stream) {
+    const unsigned blocks = (unsigned)(B * H * segments);
+    if (segments > 1) {   // walk 0, and of the two that go back, which have one state, walk 2
+        const LinearWalks states{{walks.walk[0], walks.walk[2], walks.walk[2]}};
+        const int n = backward ? 2 : 1;
+        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, true>), dim3(blocks, n), dim3(2 * D), 0, stream, states, log_decay, offsets, H, segments, segment_rows, carried);
+        hipLaunchKernelGGL(linear_carry_kernel, dim3((unsigned)(B * H * (D * D / 1024)), n), dim3(256), 0, stream, states, log_decay, offsets, H, D, segments, segment_rows,
+                           carried);
     }
-    if (states) hipLaunchKernelGGL((linear_walk_kernel<T, D, kExact, false>), grid, threads, 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
-    else hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, false>), grid, threads, 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
+    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, false>), dim3(blocks), dim3(2 * D), 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
+    if (backward)
+        hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
+}
+template <typename T, int D>
+static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H, int segments,
+                               int segment_rows, float *carried, hipStream_t stream) {
+    if constexpr (sizeof(T) == 4) launch_walks<T, D, 1>(walks, backward, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
+    else if (states) launch_walks<T, D, 3>(walks, backward, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
+    else launch_walks<T, D, 2>(walks, backward, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
     return hipGetLastError();
 }
 
 template <typename T>
-static hipError_t launch_walks(const LinearWalks &walks, int n_walks, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H, int D,
+static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H, int D,
                                int segments, int segment_rows, float *carried, hipStream_t stream) {
     switch (D) {
-        case 32: return launch_walks<T, 32>(walks, n_walks, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
-        case 64: return launch_walks<T, 64>(walks, n_walks, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
-        case 128: return launch_walks<T, 128>(walks, n_walks, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
+        case 32: return launch_walks<T, 32>(walks, backward, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
+        case 64: return launch_walks<T, 64>(walks, backward, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
+        case 128: return launch_walks<T, 128>(walks, backward, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
         default: return hipErrorInvalidValue;
     }
 }
 
-hipError_t launch_linear_walks(bool f32, const LinearWalks &walks, int n_walks, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
+hipError_t launch_linear_walks(bool f32, const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
                                int D, int segments, int segment_rows, float *carried, hipStream_t stream) {
-    return f32 ? launch_walks<float>(walks, n_walks, states, log_decay, offsets, B, H, D, segments, segment_rows, carried, stream)
-               : launch_walks<__bf16>(walks, n_walks, states, log_decay, offsets, B, H, D, segments, segment_rows, carried, stream);
+    return f32 ? launch_walks<float>(walks, backward, states, log_decay, offsets, B, H, D, segments, segment_rows, carried, stream)
+               : launch_walks<__bf16>(walks, backward, states, log_decay, offsets, B, H, D, segments, segment_rows, carried, stream);
 }
 
 template <typename T>
