@@ -2,10 +2,12 @@
 //   out_i = scale table[id_i],   dtable[v] = scale sum over the i with id_i = v of dout_i
 // The lookup is a copy of rows: bound by HBM, 16 bytes per lane, several rows of a lane in flight.
 // The gradient adds the rows of an id in the order of their positions, so that it is the same every time: the positions are sorted by id (radix
-// sort, stable, of (id, position) pairs of eight bytes: a few per cent of the rows' bytes), and every row of the table is then written
-// once, the sum of its positions' rows or zeros.  Frequent ids (one that stands for anything unknown may have a third of all positions) would
-// keep one row's lanes busy long after the others: blocks of 64 sorted positions that all have one id are added beforehand, each by lanes of its own, and
-// blocks of 64 such blocks from those, so that a row adds at most 63 single rows, 63 blocks and the blocks of blocks at either end.
+// sort, stable, of (id, position) pairs of eight bytes: a few per cent of the rows' bytes), and every row of dout is then read once, in that order.
+// The sorted positions are cut into blocks of kEmBlock, so that no id, however frequent (one that stands for anything unknown may
+// have a third of all positions), keeps one row's lanes busy long after the others: what of a block belongs to an id with positions in other blocks is
+// left as a partial sum, and those are added by the lanes of the block that the id begins in, kEmSuper of them at once where one
+// id has that many.  The table's other rows are zeros: the sort, a few dozen workgroups that wait for memory, has the chip to itself, so its launches
+// carry workgroups that clear the whole table (a row that is written again costs less than finding out that it will be).
 #include "jfa_common.h"
 #include "jfa_mfma.h"
 
@@ -15,8 +17,10 @@ namespace {
 
 constexpr int kEmThreads = 256;
 constexpr int kEmTile = 4096;    // positions that a workgroup sorts at a time
-constexpr int kEmBlock = 64;     // positions of a block, blocks of a block of blocks
+constexpr int kEmBlock = 32;     // sorted positions of a block
+constexpr int kEmSuper = 64;     // blocks that are added at once
 constexpr int kEmMostBits = 10;  // of a sort's digit
+constexpr int kSortThreads = 1024;
 
 template <typename T, int VEC> struct EmVec { typedef T Type __attribute__((ext_vector_type(VEC))); };
 template <typename T> struct EmVec<T, 1> { typedef T Type; };
@@ -91,25 +95,43 @@ template <bool FIRST> __device__ inline uint32_t sort_key(const SortSource &s, i
     return i < there && id >= 0 && id < s.V ? (uint32_t)id : (uint32_t)s.V;
 }
 
-// counts[bin * tiles + tile]; the first pass also clears the table rows' bounds.
+// What the workgroups behind a sort's own clear: `bytes` bytes from `dst` on, the ones of this launch from `from` to `to` (in units of kClearBytes).
+struct Clearing {
+    char *dst;
+    int64_t bytes, from, to;
+};
+constexpr int kClearBytes = kSortThreads * 16 * 4;
+__device__ inline void clear_share(const Clearing &c, int64_t unit) {
+    if (unit >= c.to) return;
+    const int64_t at = unit * kClearBytes;
+    if (((uintptr_t)c.dst & 15) == 0 && at + kClearBytes <= c.bytes) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) *reinterpret_cast<u32x4 *>(c.dst + at + (u * kSortThreads + threadIdx.x) * 16) = u32x4{0, 0, 0, 0};
+        return;
+    }
+    for (int64_t i = at + threadIdx.x * 2; i < at + kClearBytes && i < c.bytes; i += kSortThreads * 2) *reinterpret_cast<uint16_t *>(c.dst + i) = 0;
+}
+
+// counts[bin * tiles + tile].
 template <bool FIRST>
-__global__ __launch_bounds__(kEmThreads) void sort_count_kernel(SortSource s, int shift, int bits, int tiles, uint32_t *__restrict__ counts, uint32_t *__restrict__ bounds) {
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortSource s, int shift, int bits, int tiles, uint32_t *__restrict__ counts, Clearing clearing) {
     __shared__ uint32_t bins[1 << kEmMostBits];
+    if ((int)blockIdx.x >= tiles) return clear_share(clearing, clearing.from + blockIdx.x - tiles);
     const int n_bins = 1 << bits;
-    for (int i = threadIdx.x; i < n_bins; i += kEmThreads) bins[i] = 0;
+    for (int i = threadIdx.x; i < n_bins; i += kSortThreads) bins[i] = 0;
     __syncthreads();
     const int64_t there = FIRST ? em_rows_there(s.offsets, s.B, s.rows) : 0;
     const int first = (int)blockIdx.x * kEmTile, end = s.rows - first < kEmTile ? s.rows : first + kEmTile;
-    for (int i = first + threadIdx.x; i < end; i += kEmThreads) atomicAdd(&bins[(sort_key<FIRST>(s, there, i) >> shift) & (n_bins - 1)], 1u);
-    if (FIRST)
-        for (int64_t i = (int64_t)blockIdx.x * kEmThreads + threadIdx.x; i < 2 * s.V; i += (int64_t)gridDim.x * kEmThreads) bounds[i] = 0;
+    for (int i = first + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&bins[(sort_key<FIRST>(s, there, i) >> shift) & (n_bins - 1)], 1u);
     __syncthreads();
-    for (int i = threadIdx.x; i < n_bins; i += kEmThreads) counts[(int64_t)i * tiles + blockIdx.x] = bins[i];
+    for (int i = threadIdx.x; i < n_bins; i += kSortThreads) counts[(int64_t)i * tiles + blockIdx.x] = bins[i];
 }
 
 // A wave per bin: counts -> the counts of the tiles before, and the bin's total.
-__global__ __launch_bounds__(kEmThreads) void sort_scan_kernel(int n_bins, int tiles, uint32_t *__restrict__ counts, uint32_t *__restrict__ totals) {
-    const int bin = blockIdx.x * (kEmThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+__global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(int n_bins, int tiles, uint32_t *__restrict__ counts, uint32_t *__restrict__ totals, Clearing clearing) {
+    const int own = (n_bins + kSortThreads / 64 - 1) / (kSortThreads / 64);
+    if ((int)blockIdx.x >= own) return clear_share(clearing, clearing.from + blockIdx.x - own);
+    const int bin = blockIdx.x * (kSortThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (bin >= n_bins) return;
     uint32_t *row = counts + (int64_t)bin * tiles, carry = 0;
     for (int t0 = 0; t0 < tiles; t0 += 64) {
@@ -126,38 +148,39 @@ __global__ __launch_bounds__(kEmThreads) void sort_scan_kernel(int n_bins, int t
     if (lane == 0) totals[bin] = carry;
 }
 
-// Every key and position to its place.  A wave has a quarter of the tile in order; equal digits of a wave's 64 keys are ranked by ballots.
+// Every key and position to its place.  A wave has a sixteenth of the tile in order; equal digits of a wave's 64 keys are ranked by ballots.
+// counts and totals may be null where there is one tile.
 template <bool FIRST>
-__global__ __launch_bounds__(kEmThreads) void sort_place_kernel(SortSource s, int shift, int bits, int tiles, const uint32_t *__restrict__ counts,
-                                                                const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys, uint32_t *__restrict__ positions) {
-    constexpr int kWaves = kEmThreads / 64, kMine = kEmTile / kWaves, kRounds = kMine / 64;
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, int shift, int bits, int tiles, const uint32_t *__restrict__ counts,
+                                                                  const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys, uint32_t *__restrict__ positions,
+                                                                  Clearing clearing) {
+    constexpr int kWaves = kSortThreads / 64, kMine = kEmTile / kWaves, kRounds = kMine / 64;
     __shared__ uint32_t next[kWaves][1 << kEmMostBits];
     __shared__ uint32_t wave_totals[kWaves];
+    if ((int)blockIdx.x >= tiles) return clear_share(clearing, clearing.from + blockIdx.x - tiles);
     const int n_bins = 1 << bits, mask = n_bins - 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t there = FIRST ? em_rows_there(s.offsets, s.B, s.rows) : 0;
-    for (int i = threadIdx.x; i < n_bins; i += kEmThreads)
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) next[w][i] = 0;
-    __syncthreads();
+    for (int i = threadIdx.x; i < n_bins * kWaves; i += kSortThreads) next[i >> bits][i & mask] = 0;
     const int first = (int)blockIdx.x * kEmTile + wave * kMine;
     uint32_t key[kRounds];
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-        const int i = first + r * 64 + lane;
-        key[r] = 0;
-        if (i < s.rows) {
-            key[r] = sort_key<FIRST>(s, there, i);
-            atomicAdd(&next[wave][(key[r] >> shift) & mask], 1u);
-        }
-    }
+    for (int r = 0; r < kRounds; ++r) key[r] = first + r * 64 + lane < s.rows ? sort_key<FIRST>(s, there, first + r * 64 + lane) : 0;
     __syncthreads();
-    // where a bin starts: the totals of the bins before it; a thread has kPer bins in a row
-    const int per = n_bins / kEmThreads > 0 ? n_bins / kEmThreads : 1, bin0 = threadIdx.x * per;
-    uint32_t mine = 0;
-    if (bin0 < n_bins)
-        for (int k = 0; k < per; ++k) mine += totals[bin0 + k];
-    uint32_t sum = mine;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (first + r * 64 + lane < s.rows) atomicAdd(&next[wave][(key[r] >> shift) & mask], 1u);
+    __syncthreads();
+    // a thread per bin: what the waves have of it, then where the bin starts: behind the bins before it
+    static_assert(1 << kEmMostBits <= kSortThreads, "a thread per bin");
+    const int bin = threadIdx.x;
+    uint32_t here = 0, total = 0;
+    if (bin < n_bins) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) here += next[w][bin];
+        total = totals ? totals[bin] : here;
+    }
+    uint32_t sum = total;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t y = __shfl_up(sum, d, 64);
@@ -165,19 +188,17 @@ __global__ __launch_bounds__(kEmThreads) void sort_place_kernel(SortSource s, in
     }
     if (lane == 63) wave_totals[wave] = sum;
     __syncthreads();
-    uint32_t start = sum - mine;
-    for (int w = 0; w < wave; ++w) start += wave_totals[w];
-    if (bin0 < n_bins)
-        for (int k = 0; k < per; ++k) {
-            uint32_t at = start + counts[(int64_t)(bin0 + k) * tiles + blockIdx.x];
-            start += totals[bin0 + k];
+    uint32_t at_bin = sum - total;
+    for (int w = 0; w < wave; ++w) at_bin += wave_totals[w];
+    if (bin < n_bins) {
+        if (counts) at_bin += counts[(int64_t)bin * tiles + blockIdx.x];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const uint32_t c = next[w][bin0 + k];
-                next[w][bin0 + k] = at;
-                at += c;
-            }
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t c = next[w][bin];
+            next[w][bin] = at_bin;
+            at_bin += c;
         }
+    }
     __syncthreads();
     volatile uint32_t *const at = next[wave];   // the wave's own from here on; its LDS instructions are served in order
 #pragma unroll
@@ -204,25 +225,83 @@ __global__ __launch_bounds__(kEmThreads) void sort_place_kernel(SortSource s, in
     }
 }
 
-// bounds[2 v], bounds[2 v + 1]: the sorted positions of row v (cleared before: none).
-__global__ __launch_bounds__(kEmThreads) void bounds_kernel(const uint32_t *__restrict__ keys, int rows, uint32_t V, uint32_t *__restrict__ bounds) {
-    const int i = blockIdx.x * kEmThreads + threadIdx.x;
-    if (i >= rows) return;
-    const uint32_t key = keys[i];
-    if (key >= V) return;
-    if (i == 0 || keys[i - 1] != key) bounds[2 * (int64_t)key] = i;
-    if (i == rows - 1 || keys[i + 1] != key) bounds[2 * (int64_t)key + 1] = i + 1;
+// ---- sums of rows ----
+// Block k: sorted positions kEmBlock k up to the next block's (or the end).  An id whose positions are all inside: its row of the table.  The sum of those that
+// an earlier block's last id has in this one: heads[k]; of those of the last id, where it begins in this block and goes on in the next: tails[k].
+template <typename T, int VEC, int LANES>
+__global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restrict__ dout, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ positions, int rows,
+                                                                int n_blocks, uint32_t V, int64_t N, float scale, T *__restrict__ dtable, float *__restrict__ heads,
+                                                                float *__restrict__ tails) {
+    typedef typename EmVec<T, VEC>::Type Raw;
+    constexpr int kAhead = 8;
+    const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    if (k >= n_blocks) return;
+    const int first = k * kEmBlock, end = rows - first < kEmBlock ? rows : first + kEmBlock;
+    const uint32_t before = first > 0 ? keys[first - 1] : ~0u, after = end < rows ? keys[end] : ~0u;   // (no key is that large)
+    for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
+        uint32_t key[2][kAhead];
+        Raw row[2][kAhead];
+        auto read = [&](int from, int buffer) {
+            uint32_t at[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int r = from + u < end ? from + u : end - 1;
+                key[buffer][u] = keys[r];
+                at[u] = positions[r];
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) row[buffer][u] = *reinterpret_cast<const Raw *>(dout + (int64_t)at[u] * N + c);
+        };
+        float sum[VEC];
+        uint32_t current = keys[first];
+        bool began = current != before;   // inside this block
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
+        auto row_is_done = [&]() {
+            if (!began) em_store<float, VEC>(heads + (int64_t)k * N + c, sum);
+            else if (current < V) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] *= scale;
+                em_store<T, VEC>(dtable + (int64_t)current * N + c, sum);
+            }
+        };
+        read(first, 0);
+#pragma unroll
+        for (int batch = 0; batch < kEmBlock / kAhead; ++batch) {
+            const int from = first + batch * kAhead;
+            if (from >= end) break;
+            if (batch + 1 < kEmBlock / kAhead) read(from + kAhead, (batch + 1) & 1);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (from + u >= end) break;
+                if (key[batch & 1][u] != current) {
+                    row_is_done();
+                    current = key[batch & 1][u];
+                    began = true;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
+                }
+                const Raw x = row[batch & 1][u];
+                if constexpr (VEC == 1) sum[0] += (float)x;
+                else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[e] += (float)x[e];
+                }
+            }
+        }
+        if (began && current == after) em_store<float, VEC>(tails + (int64_t)k * N + c, sum);
+        else row_is_done();
+    }
 }
 
-// ---- sums of rows ----
-// Adds `count` rows of `src`, row r at index(r); kAhead loads in flight.
-template <typename S, int VEC, typename Index> __device__ inline void add_rows(const S *src, int64_t N, int64_t c, int from, int to, Index index, float (&sum)[VEC]) {
+// Adds rows from .. to - 1 of `src`, kAhead loads in flight.
+template <int VEC> __device__ inline void add_rows(const float *src, int64_t N, int64_t c, int from, int to, float (&sum)[VEC]) {
     constexpr int kAhead = 8;
     for (int r = from; r < to; r += kAhead) {
         float x[kAhead][VEC];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (r + u < to) em_load<S, VEC>(src + (int64_t)index(r + u) * N + c, x[u]);
+            if (r + u < to) em_load<float, VEC>(src + (int64_t)(r + u) * N + c, x[u]);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
             if (r + u < to) {
@@ -232,76 +311,56 @@ template <typename S, int VEC, typename Index> __device__ inline void add_rows(c
     }
 }
 
-// blocks[k][N]: the sum of sorted positions 64 k .. 64 k + 63 where all of them have one id.
-template <typename T, int VEC, int LANES>
-__global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restrict__ dout, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ positions,
-                                                                int n_blocks, uint32_t V, int64_t N, float *__restrict__ blocks) {
-    const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    if (k >= n_blocks) return;
-    const int first = k * kEmBlock;
-    const uint32_t key = keys[first];
-    if (key >= V || keys[first + kEmBlock - 1] != key) return;
-    for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
-        float sum[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-        add_rows<T, VEC>(dout, N, c, first, first + kEmBlock, [&](int r) { return positions[r]; }, sum);
-        em_store<float, VEC>(blocks + (int64_t)k * N + c, sum);
-    }
-}
-
-// supers[k][N]: the sum of blocks 64 k .. 64 k + 63 where all of their positions have one id.
+// supers[k]: the sum of heads kEmSuper k .. kEmSuper (k + 1) - 1, where one id has all of their positions (and is looked for where it began earlier).
 template <int VEC, int LANES>
-__global__ __launch_bounds__(kEmThreads) void super_sums_kernel(const uint32_t *__restrict__ keys, int n_supers, uint32_t V, int64_t N, const float *__restrict__ blocks,
+__global__ __launch_bounds__(kEmThreads) void super_sums_kernel(const uint32_t *__restrict__ keys, int n_supers, uint32_t V, int64_t N, const float *__restrict__ heads,
                                                                 float *__restrict__ supers) {
     const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
     if (k >= n_supers) return;
-    const int64_t first = (int64_t)k * kEmBlock * kEmBlock;
+    const int64_t first = (int64_t)k * kEmSuper * kEmBlock;
     const uint32_t key = keys[first];
-    if (key >= V || keys[first + kEmBlock * kEmBlock - 1] != key) return;
+    if (key >= V || keys[first + kEmSuper * kEmBlock - 1] != key || first == 0 || keys[first - 1] != key) return;
     for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
         float sum[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-        add_rows<float, VEC>(blocks, N, c, k * kEmBlock, (k + 1) * kEmBlock, [](int r) { return r; }, sum);
+        add_rows<VEC>(heads, N, c, k * kEmSuper, (k + 1) * kEmSuper, sum);
         em_store<float, VEC>(supers + (int64_t)k * N + c, sum);
     }
 }
 
-// dtable: LANES lanes per row of the table.
+// The rows of ids that begin in one block and end in another: LANES lanes for each block.
 template <typename T, int VEC, int LANES>
-__global__ __launch_bounds__(kEmThreads) void table_rows_kernel(const T *__restrict__ dout, const uint32_t *__restrict__ positions, const uint32_t *__restrict__ bounds,
-                                                                int64_t V, int64_t N, float scale, const float *__restrict__ blocks, const float *__restrict__ supers,
-                                                                T *__restrict__ dtable) {
-    constexpr int kPerBlock = kEmThreads / LANES;
-    const int lane = threadIdx.x % LANES;
-    for (int64_t v = (int64_t)blockIdx.x * kPerBlock + threadIdx.x / LANES; v < V; v += (int64_t)gridDim.x * kPerBlock) {
-        const int first = (int)bounds[2 * v], end = (int)bounds[2 * v + 1];
-        int block0 = (first + kEmBlock - 1) / kEmBlock, block1 = end / kEmBlock;   // the blocks inside
-        if (block0 > block1) block0 = block1 = -1;
-        int super0 = (block0 + kEmBlock - 1) / kEmBlock, super1 = block1 / kEmBlock;
-        if (block0 < 0 || super0 > super1) super0 = super1 = -1;
-        for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
-            float sum[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-            const auto position = [&](int r) { return positions[r]; };
-            const auto same = [](int r) { return r; };
-            if (block0 < 0) add_rows<T, VEC>(dout, N, c, first, end, position, sum);
-            else {
-                add_rows<T, VEC>(dout, N, c, first, block0 * kEmBlock, position, sum);
-                if (super0 < 0) add_rows<float, VEC>(blocks, N, c, block0, block1, same, sum);
-                else {
-                    add_rows<float, VEC>(blocks, N, c, block0, super0 * kEmBlock, same, sum);
-                    add_rows<float, VEC>(supers, N, c, super0, super1, same, sum);
-                    add_rows<float, VEC>(blocks, N, c, super1 * kEmBlock, block1, same, sum);
-                }
-                add_rows<T, VEC>(dout, N, c, block1 * kEmBlock, end, position, sum);
-            }
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-            em_store<T, VEC>(dtable + v * N + c, sum);
+__global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t *__restrict__ keys, int n_blocks, uint32_t V, int64_t N, float scale,
+                                                                 const float *__restrict__ heads, const float *__restrict__ tails, const float *__restrict__ supers,
+                                                                 T *__restrict__ dtable) {
+    const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    if (k + 1 >= n_blocks) return;   // (the last block's ids end in it)
+    const int64_t next = (int64_t)(k + 1) * kEmBlock;
+    const uint32_t key = keys[next - 1];
+    if (key >= V || keys[next] != key || (k > 0 && keys[next - kEmBlock - 1] == key)) return;
+    // the last block whose first position is the id's: doubling steps, then halving ones
+    int last = k + 1, step = 1;
+    while (last + step < n_blocks && keys[(int64_t)(last + step) * kEmBlock] == key) {
+        last += step;
+        step *= 2;
+    }
+    for (; step > 0; step /= 2)
+        if (last + step < n_blocks && keys[(int64_t)(last + step) * kEmBlock] == key) last += step;
+    // heads k + 1 .. last; those of whole supers in front of the last block (whose positions need not all be the id's) come from there
+    int super0 = (k + 1 + kEmSuper - 1) / kEmSuper, super1 = last / kEmSuper;
+    const bool any = super0 < super1;
+    for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
+        float sum[VEC];
+        em_load<float, VEC>(tails + (int64_t)k * N + c, sum);
+        add_rows<VEC>(heads, N, c, k + 1, any ? super0 * kEmSuper : last + 1, sum);
+        if (any) {
+            add_rows<VEC>(supers, N, c, super0, super1, sum);
+            add_rows<VEC>(heads, N, c, super1 * kEmSuper, last + 1, sum);
         }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] *= scale;
+        em_store<T, VEC>(dtable + (int64_t)key * N + c, sum);
     }
 }
 
@@ -335,7 +394,7 @@ hipError_t embedding_t(const T *table, const Id *ids, const int64_t *offsets, in
 struct EmPlan {
     int bits, passes, tiles;
     int n_blocks, n_supers;
-    int64_t counts, totals, bounds, keys[2], positions[2], blocks, supers, words;
+    int64_t counts, totals, keys[2], positions[2], heads, tails, supers, words;
 };
 EmPlan em_plan(int64_t rows, int64_t V, int64_t N) {
     EmPlan p;
@@ -343,16 +402,16 @@ EmPlan em_plan(int64_t rows, int64_t V, int64_t N) {
     while (((int64_t)1 << bits) < V + 1) ++bits;   // keys 0 .. V
     p.passes = (bits + kEmMostBits - 1) / kEmMostBits;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.tiles = rows > 0 ? (int)((rows + kEmTile - 1) / kEmTile) : 1;   // (no rows: one tile with nothing in it)
-    p.n_blocks = (int)(rows / kEmBlock);
-    p.n_supers = (int)(rows / (kEmBlock * kEmBlock));
+    p.tiles = (int)((rows + kEmTile - 1) / kEmTile);
+    p.n_blocks = (int)((rows + kEmBlock - 1) / kEmBlock);
+    p.n_supers = (int)(rows / (kEmBlock * kEmSuper));
     int64_t at = 0;
     const auto take = [&](int64_t words) { const int64_t here = at; at += (words + 3) / 4 * 4; return here; };
     p.counts = take((int64_t)p.tiles << p.bits);
     p.totals = take((int64_t)1 << p.bits);
-    p.bounds = take(2 * V);
     for (int i = 0; i < 2; ++i) { p.keys[i] = take(rows); p.positions[i] = take(rows); }
-    p.blocks = take(p.n_blocks * N);
+    p.heads = take(p.n_blocks * N);
+    p.tails = take(p.n_blocks * N);
     p.supers = take(p.n_supers * N);
     p.words = at;
     return p;
@@ -362,31 +421,49 @@ template <typename T>
 hipError_t embedding_backward_t(const T *dout, const void *ids, bool ids64, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale,
                                 T *dtable, uint32_t *ws, hipStream_t stream) {
     const EmPlan p = em_plan(rows, V, N);
-    const dim3 threads(kEmThreads);
-    uint32_t *const counts = ws + p.counts, *const totals = ws + p.totals, *const bounds = ws + p.bounds;
+    const dim3 threads(kSortThreads);
+    uint32_t *const counts = p.tiles > 1 ? ws + p.counts : nullptr, *const totals = p.tiles > 1 ? ws + p.totals : nullptr;
     SortSource s{ids, nullptr, nullptr, offsets, B, V, (int)rows, ids64};
+    // every launch of the sort clears a share of the table
+    const int64_t table_bytes = V * N * (int64_t)sizeof(T), units = (table_bytes + kClearBytes - 1) / kClearBytes;
+    const int launches = p.passes * (p.tiles > 1 ? 3 : 1);
+    int launch = 0;
+    const auto share = [&]() {
+        const Clearing c{(char *)dtable, table_bytes, units * launch / launches, units * (launch + 1) / launches};
+        ++launch;
+        return c;
+    };
+    const auto grid = [](int own, const Clearing &c) { return dim3((unsigned)(own + c.to - c.from)); };
+    if (rows == 0) {
+        const Clearing c{(char *)dtable, table_bytes, 0, units};
+        hipLaunchKernelGGL((sort_count_kernel<true>), grid(0, c), threads, 0, stream, s, 0, 1, 0, nullptr, c);
+        return hipGetLastError();
+    }
     for (int pass = 0; pass < p.passes; ++pass) {
         uint32_t *const keys = ws + p.keys[pass & 1], *const positions = ws + p.positions[pass & 1];
-        const int shift = pass * p.bits;
-        if (pass == 0) hipLaunchKernelGGL((sort_count_kernel<true>), dim3(p.tiles), threads, 0, stream, s, shift, p.bits, p.tiles, counts, bounds);
-        else hipLaunchKernelGGL((sort_count_kernel<false>), dim3(p.tiles), threads, 0, stream, s, shift, p.bits, p.tiles, counts, bounds);
-        hipLaunchKernelGGL(sort_scan_kernel, dim3(((1 << p.bits) + 3) / 4), threads, 0, stream, 1 << p.bits, p.tiles, counts, totals);
-        if (pass == 0) hipLaunchKernelGGL((sort_place_kernel<true>), dim3(p.tiles), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions);
-        else hipLaunchKernelGGL((sort_place_kernel<false>), dim3(p.tiles), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions);
+        const int shift = pass * p.bits, bins = 1 << p.bits;
+        if (p.tiles > 1) {
+            const Clearing c = share();
+            if (pass == 0) hipLaunchKernelGGL((sort_count_kernel<true>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, c);
+            else hipLaunchKernelGGL((sort_count_kernel<false>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, c);
+            const Clearing d = share();
+            hipLaunchKernelGGL(sort_scan_kernel, grid((bins + kSortThreads / 64 - 1) / (kSortThreads / 64), d), threads, 0, stream, bins, p.tiles, counts, totals, d);
+        }
+        const Clearing c = share();
+        if (pass == 0) hipLaunchKernelGGL((sort_place_kernel<true>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions, c);
+        else hipLaunchKernelGGL((sort_place_kernel<false>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions, c);
         s.keys = keys;
         s.positions = positions;
     }
-    hipLaunchKernelGGL(bounds_kernel, dim3((unsigned)(rows / kEmThreads + 1)), threads, 0, stream, s.keys, (int)rows, (uint32_t)V, bounds);
-    float *const blocks = reinterpret_cast<float *>(ws + p.blocks), *const supers = reinterpret_cast<float *>(ws + p.supers);
+    float *const heads = reinterpret_cast<float *>(ws + p.heads), *const tails = reinterpret_cast<float *>(ws + p.tails), *const supers = reinterpret_cast<float *>(ws + p.supers);
     return em_spread<T>(N, aligned16(dout, dtable), [&](auto vec, auto lanes) {
         constexpr int VEC = decltype(vec)::value, L = decltype(lanes)::value, kPer = kEmThreads / L;
-        if (p.n_blocks)
-            hipLaunchKernelGGL((block_sums_kernel<T, VEC, L>), dim3((p.n_blocks + kPer - 1) / kPer), threads, 0, stream, dout, s.keys, s.positions, p.n_blocks, (uint32_t)V, N, blocks);
+        const dim3 blocks((p.n_blocks + kPer - 1) / kPer), few(kEmThreads);
+        hipLaunchKernelGGL((block_sums_kernel<T, VEC, L>), blocks, few, 0, stream, dout, s.keys, s.positions, (int)rows, p.n_blocks, (uint32_t)V, N, scale, dtable, heads, tails);
         if (p.n_supers)
-            hipLaunchKernelGGL((super_sums_kernel<VEC, L>), dim3((p.n_supers + kPer - 1) / kPer), threads, 0, stream, s.keys, p.n_supers, (uint32_t)V, N, blocks, supers);
-        const int64_t need = (V + kPer - 1) / kPer;
-        hipLaunchKernelGGL((table_rows_kernel<T, VEC, L>), dim3((unsigned)(need < 65536 ? need : 65536)), threads, 0, stream, dout, s.positions, bounds, V, N, scale, blocks,
-                           supers, dtable);
+            hipLaunchKernelGGL((super_sums_kernel<VEC, L>), dim3((p.n_supers + kPer - 1) / kPer), few, 0, stream, s.keys, p.n_supers, (uint32_t)V, N, heads, supers);
+        if (p.n_blocks > 1)
+            hipLaunchKernelGGL((join_blocks_kernel<T, VEC, L>), blocks, few, 0, stream, s.keys, p.n_blocks, (uint32_t)V, N, scale, heads, tails, supers, dtable);
         return hipGetLastError();
     });
 }
