@@ -238,26 +238,33 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
     if (k >= n_blocks) return;
     const int first = k * kEmBlock, end = rows - first < kEmBlock ? rows : first + kEmBlock;
     const uint32_t before = first > 0 ? keys[first - 1] : ~0u, after = end < rows ? keys[end] : ~0u;   // (no key is that large)
-    for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
-        uint32_t key[2][kAhead];
+    // the block's keys and positions, kEach of them with every lane: read once, so that nothing but the rows themselves is waited for below
+    constexpr int kEach = LANES < kEmBlock ? kEmBlock / LANES : 1;
+    uint32_t my_key[kEach], my_position[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int r = first + i * LANES + lane < end ? first + i * LANES + lane : end - 1;
+        my_key[i] = keys[r];
+        my_position[i] = positions[r];
+    }
+    const auto of = [&](const uint32_t (&x)[kEach], int r) { return (uint32_t)__shfl((int)x[r / LANES], r % LANES, LANES); };   // r: a constant
+    for (int64_t c = lane * VEC; c - lane * VEC < N; c += LANES * VEC) {   // (every lane takes part in the exchanges)
+        const bool mine = c < N;
         Raw row[2][kAhead];
         auto read = [&](int from, int buffer) {
-            uint32_t at[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int r = from + u < end ? from + u : end - 1;
-                key[buffer][u] = keys[r];
-                at[u] = positions[r];
+                const uint32_t at = of(my_position, from + u);
+                if (mine) row[buffer][u] = *reinterpret_cast<const Raw *>(dout + (int64_t)at * N + c);
             }
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) row[buffer][u] = *reinterpret_cast<const Raw *>(dout + (int64_t)at[u] * N + c);
         };
         float sum[VEC];
-        uint32_t current = keys[first];
+        uint32_t current = of(my_key, 0);
         bool began = current != before;   // inside this block
 #pragma unroll
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
         auto row_is_done = [&]() {
+            if (!mine) return;
             if (!began) em_store<float, VEC>(heads + (int64_t)k * N + c, sum);
             else if (current < V) {
 #pragma unroll
@@ -265,18 +272,18 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
                 em_store<T, VEC>(dtable + (int64_t)current * N + c, sum);
             }
         };
-        read(first, 0);
+        read(0, 0);
 #pragma unroll
         for (int batch = 0; batch < kEmBlock / kAhead; ++batch) {
-            const int from = first + batch * kAhead;
-            if (from >= end) break;
-            if (batch + 1 < kEmBlock / kAhead) read(from + kAhead, (batch + 1) & 1);
+            if (first + batch * kAhead >= end) break;
+            if (batch + 1 < kEmBlock / kAhead) read((batch + 1) * kAhead, (batch + 1) & 1);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (from + u >= end) break;
-                if (key[batch & 1][u] != current) {
+                const uint32_t key = of(my_key, batch * kAhead + u);
+                if (first + batch * kAhead + u >= end) break;
+                if (key != current) {
                     row_is_done();
-                    current = key[batch & 1][u];
+                    current = key;
                     began = true;
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
@@ -289,8 +296,8 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
                 }
             }
         }
-        if (began && current == after) em_store<float, VEC>(tails + (int64_t)k * N + c, sum);
-        else row_is_done();
+        if (!began || current != after) row_is_done();
+        else if (mine) em_store<float, VEC>(tails + (int64_t)k * N + c, sum);
     }
 }
 
@@ -311,56 +318,115 @@ template <int VEC> __device__ inline void add_rows(const float *src, int64_t N, 
     }
 }
 
-// supers[k]: the sum of heads kEmSuper k .. kEmSuper (k + 1) - 1, where one id has all of their positions (and is looked for where it began earlier).
+// The sum of what the kPer lane groups of a workgroup have each added, in their order, with the first of them; `slots`: VEC floats a thread.
+template <int VEC, int LANES> __device__ inline void groups_sum(float (&sum)[VEC], float (*slots)[VEC]) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) slots[threadIdx.x][e] = sum[e];
+    __syncthreads();
+    if (threadIdx.x < LANES)
+        for (int g = 1; g < kEmThreads / LANES; ++g)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[e] += slots[g * LANES + threadIdx.x][e];
+}
+
+// supers[k]: the sum of heads kEmSuper k .. kEmSuper (k + 1) - 1, where one id has all of their positions and began earlier.  A workgroup each.
 template <int VEC, int LANES>
-__global__ __launch_bounds__(kEmThreads) void super_sums_kernel(const uint32_t *__restrict__ keys, int n_supers, uint32_t V, int64_t N, const float *__restrict__ heads,
+__global__ __launch_bounds__(kEmThreads) void super_sums_kernel(const uint32_t *__restrict__ keys, uint32_t V, int64_t N, const float *__restrict__ heads,
                                                                 float *__restrict__ supers) {
-    const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    if (k >= n_supers) return;
+    constexpr int kPer = kEmThreads / LANES, kEach = kEmSuper > kPer ? kEmSuper / kPer : 1;   // heads of a lane group
+    __shared__ float slots[kEmThreads][VEC];
+    const int k = blockIdx.x, group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     const int64_t first = (int64_t)k * kEmSuper * kEmBlock;
     const uint32_t key = keys[first];
     if (key >= V || keys[first + kEmSuper * kEmBlock - 1] != key || first == 0 || keys[first - 1] != key) return;
-    for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
+    for (int64_t c = lane * VEC; c - lane * VEC < N; c += LANES * VEC) {
         float sum[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-        add_rows<VEC>(heads, N, c, k * kEmSuper, (k + 1) * kEmSuper, sum);
-        em_store<float, VEC>(supers + (int64_t)k * N + c, sum);
+        if (c < N && group * kEach < kEmSuper) add_rows<VEC>(heads, N, c, k * kEmSuper + group * kEach, k * kEmSuper + (group + 1) * kEach, sum);
+        groups_sum<VEC, LANES>(sum, slots);
+        if (group == 0 && c < N) em_store<float, VEC>(supers + (int64_t)k * N + c, sum);
     }
 }
 
-// The rows of ids that begin in one block and end in another: LANES lanes for each block.
+// The rows of ids that begin in one block and end in another.  A workgroup has a block for each of its groups of LANES lanes; ids with more
+// than kFewHeads heads are added by all of them together.
 template <typename T, int VEC, int LANES>
 __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t *__restrict__ keys, int n_blocks, uint32_t V, int64_t N, float scale,
                                                                  const float *__restrict__ heads, const float *__restrict__ tails, const float *__restrict__ supers,
                                                                  T *__restrict__ dtable) {
-    const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    if (k + 1 >= n_blocks) return;   // (the last block's ids end in it)
+    constexpr int kPer = kEmThreads / LANES, kFewHeads = 16;
+    __shared__ float slots[kEmThreads][VEC];
+    __shared__ int long_block[kPer], long_last[kPer];
+    const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, k = blockIdx.x * kPer + group;
     const int64_t next = (int64_t)(k + 1) * kEmBlock;
-    const uint32_t key = keys[next - 1];
-    if (key >= V || keys[next] != key || (k > 0 && keys[next - kEmBlock - 1] == key)) return;
-    // the last block whose first position is the id's: doubling steps, then halving ones
-    int last = k + 1, step = 1;
-    while (last + step < n_blocks && keys[(int64_t)(last + step) * kEmBlock] == key) {
-        last += step;
-        step *= 2;
+    uint32_t key = V;
+    if (k + 1 < n_blocks) {   // (the last block's ids end in it)
+        key = keys[next - 1];
+        if (key < V && (keys[next] != key || (k > 0 && keys[next - kEmBlock - 1] == key))) key = V;
     }
-    for (; step > 0; step /= 2)
-        if (last + step < n_blocks && keys[(int64_t)(last + step) * kEmBlock] == key) last += step;
-    // heads k + 1 .. last; those of whole supers in front of the last block (whose positions need not all be the id's) come from there
-    int super0 = (k + 1 + kEmSuper - 1) / kEmSuper, super1 = last / kEmSuper;
-    const bool any = super0 < super1;
-    for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
-        float sum[VEC];
-        em_load<float, VEC>(tails + (int64_t)k * N + c, sum);
-        add_rows<VEC>(heads, N, c, k + 1, any ? super0 * kEmSuper : last + 1, sum);
-        if (any) {
-            add_rows<VEC>(supers, N, c, super0, super1, sum);
-            add_rows<VEC>(heads, N, c, super1 * kEmSuper, last + 1, sum);
+    int last = k;   // the last block whose first position is the id's: block k + 1 is one, and then LANES blocks are looked at at a time
+    if (key < V) {
+        last = k + 1;
+        int step = 1;
+        for (;;) {
+            const int64_t probe = (int64_t)last + (int64_t)(lane + 1) * step;
+            const bool is = probe < n_blocks && keys[probe * kEmBlock] == key;   // true for a prefix of the lanes
+            const uint64_t votes = __builtin_amdgcn_ballot_w64(is) >> ((threadIdx.x & 63) / LANES * LANES);
+            const int hits = __popcll(LANES == 64 ? votes : votes & ((1ull << (LANES & 63)) - 1));
+            last += hits * step;
+            if (hits == LANES) step *= LANES;        // the end is farther away
+            else if (step > 1) step /= LANES;        // it is less than a step away
+            else break;
         }
+    }
+    const bool many = last - k > kFewHeads;
+    if (lane == 0) {
+        long_block[group] = many ? k : -1;
+        long_last[group] = last;
+    }
+    __syncthreads();
+    if (key < V && !many)
+        for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
+            float sum[VEC];
+            em_load<float, VEC>(tails + (int64_t)k * N + c, sum);
+            add_rows<VEC>(heads, N, c, k + 1, last + 1, sum);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-        em_store<T, VEC>(dtable + (int64_t)key * N + c, sum);
+            for (int e = 0; e < VEC; ++e) sum[e] *= scale;
+            em_store<T, VEC>(dtable + (int64_t)key * N + c, sum);
+        }
+    for (int g = 0; g < kPer; ++g) {
+        const int b = long_block[g], end = long_last[g];
+        if (b < 0) continue;
+        // heads b + 1 .. end; those of whole supers in front of block `end` (whose positions need not all be the id's) come from there
+        const int super0 = (b + 1 + kEmSuper - 1) / kEmSuper, super1 = end / kEmSuper;
+        const bool any = super0 < super1;
+        const int head1 = any ? super0 * kEmSuper : end + 1;   // heads b + 1 .. head1 - 1, then supers, then heads super1 * kEmSuper .. end
+        const uint32_t id = keys[(int64_t)(b + 1) * kEmBlock];
+        for (int64_t c = lane * VEC; c - lane * VEC < N; c += LANES * VEC) {
+            float sum[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
+            if (c < N) {
+                const auto part = [&](const float *src, int from, int to) {   // this group's
+                    const int each = (to - from + kPer - 1) / kPer, mine = from + group * each;
+                    add_rows<VEC>(src, N, c, mine, mine + each < to ? mine + each : to, sum);
+                };
+                if (group == 0) em_load<float, VEC>(tails + (int64_t)b * N + c, sum);
+                part(heads, b + 1, head1);
+                if (any) {
+                    part(supers, super0, super1);
+                    part(heads, super1 * kEmSuper, end + 1);
+                }
+            }
+            groups_sum<VEC, LANES>(sum, slots);
+            if (group == 0 && c < N) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] *= scale;
+                em_store<T, VEC>(dtable + (int64_t)id * N + c, sum);
+            }
+        }
     }
 }
 
@@ -461,7 +527,7 @@ hipError_t embedding_backward_t(const T *dout, const void *ids, bool ids64, cons
         const dim3 blocks((p.n_blocks + kPer - 1) / kPer), few(kEmThreads);
         hipLaunchKernelGGL((block_sums_kernel<T, VEC, L>), blocks, few, 0, stream, dout, s.keys, s.positions, (int)rows, p.n_blocks, (uint32_t)V, N, scale, dtable, heads, tails);
         if (p.n_supers)
-            hipLaunchKernelGGL((super_sums_kernel<VEC, L>), dim3((p.n_supers + kPer - 1) / kPer), few, 0, stream, s.keys, p.n_supers, (uint32_t)V, N, heads, supers);
+            hipLaunchKernelGGL((super_sums_kernel<VEC, L>), dim3(p.n_supers), few, 0, stream, s.keys, (uint32_t)V, N, heads, supers);
         if (p.n_blocks > 1)
             hipLaunchKernelGGL((join_blocks_kernel<T, VEC, L>), blocks, few, 0, stream, s.keys, p.n_blocks, (uint32_t)V, N, scale, heads, tails, supers, dtable);
         return hipGetLastError();
