@@ -139,7 +139,8 @@ def _load_native():
             _native = False
             return
         lib = binding.load()
-        nodes.bind_library(lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value, binding._check, binding._ptr)
+        nodes.bind_library(lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value, binding._check, binding._ptr,
+                           torch.nn.Parameter)
         _native = nodes
 
 
@@ -151,6 +152,15 @@ def _ordinary(*tensors) -> bool:
         _load_native()
     return (_native is not False and all(type(t) in _PLAIN for t in tensors) and torch._C._get_tracing_state() is None
             and not torch._C._are_functorch_transforms_active() and forward_ad._current_level < 0)
+
+
+def _nodes():
+    """The C++ functions, None where a call is not theirs whatever its arguments (they look at those themselves)."""
+    if torch.compiler.is_compiling() or forward_ad._current_level >= 0:
+        return None
+    if _native is None:
+        _load_native()
+    return _native or None
 
 
 def jagged_flash_attention(q, k, v, offsets, max_len: int, causal: bool = False):
@@ -179,16 +189,23 @@ def jagged_linear_attention(q, k, v, log_decay, offsets, max_len: int, scale=Non
     final states too, as a second result.  Gradients flow to the states as well, not to log_decay."""
     if log_decay.requires_grad:
         raise ValueError("jagged_linear_attention: log_decay is not differentiable")
-    return _LinearAttention.apply(q, k, v, log_decay, offsets, int(max_len), q.shape[-1] ** -0.5 if scale is None else float(scale), initial_state, bool(return_state))
+    args = (q, k, v, log_decay, offsets, int(max_len), q.shape[-1] ** -0.5 if scale is None else float(scale), initial_state, bool(return_state))
+    if (nodes := _nodes()) and (result := nodes.linear_attention(*args)) is not None:   # None: not in order, the function below says what is wrong
+        return result
+    return _LinearAttention.apply(*args)
 
 
 def jagged_layer_norm(x, weight=None, bias=None, offsets=None, eps: float = 1e-5):
     """Layer norm over the last dimensions of x [rows, ...], those of weight and bias (without either the last one).  offsets: of
     the rows only the first offsets[B] are there."""
+    if (nodes := _nodes()) and (y := nodes.layer_norm(x, weight, bias, offsets, float(eps))) is not None:
+        return y
     return _LayerNorm.apply(x, weight, bias, offsets, float(eps))
 
 
 def jagged_embedding(table, ids, offsets=None, scale: float = 1.0):
     """scale table[ids] for table [V, ...] and ids [rows] (int64 or int32), zeros for an id outside the table.  offsets: of the
     rows only the first offsets[B] are there."""
+    if (nodes := _nodes()) and (out := nodes.embedding(table, ids, offsets, float(scale))) is not None:
+        return out
     return _Embedding.apply(table, ids, offsets, float(scale))

@@ -448,6 +448,11 @@ def _workspace(n_bytes: int, device) -> Optional[torch.Tensor]:
     return torch.empty(n_bytes, dtype=torch.uint8, device=device) if n_bytes else None
 
 
+def _row_ptr(t: Optional[torch.Tensor], offsets: torch.Tensor) -> Optional[int]:
+    """The address of a tensor of rows.  A tensor without rows has none, and its samples are all empty: any address will do then."""
+    return _ptr(offsets) if t is not None and t.numel() == 0 and t.is_cuda else _ptr(t)
+
+
 def _check_linear(q, k, v, log_decay, batch: Optional[int], *states):
     assert q.dim() == 3 and k.shape == q.shape and v.shape == q.shape and k.dtype == q.dtype and v.dtype == q.dtype
     _, H, D = q.shape
@@ -475,7 +480,8 @@ def jfa_linear_attention(q, k, v, log_decay, offsets, max_len: int, scale: Optio
             final_state = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
         workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, max_len, H, D, 0), q.device)
         _check(_pick(q.dtype, "jfa_linear_attention")(
-            _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale, _ptr(initial_state), _ptr(out),
+            *(_row_ptr(t, offsets) for t in (q, k, v)), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale, _ptr(initial_state),
+            _row_ptr(out, offsets),
             _ptr(final_state), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
     return out, final_state
 
@@ -493,16 +499,18 @@ def jfa_linear_attention_backward(q, k, v, dout, log_decay, offsets, max_len: in
             dinitial_state = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
         workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, max_len, H, D, 1), q.device)
         _check(_pick(q.dtype, "jfa_linear_attention_backward")(
-            _ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale, _ptr(initial_state),
-            _ptr(dfinal_state), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dinitial_state), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+            *(_row_ptr(t, offsets) for t in (q, k, v, dout)), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale,
+            _ptr(initial_state), _ptr(dfinal_state), *(_row_ptr(t, offsets) for t in (dq, dk, dv)), _ptr(dinitial_state), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
     return dq, dk, dv, dinitial_state
 
 
 def jfa_linear_attention_step(q, k, v, log_decay, state, scale: Optional[float] = None, out=None, new_state=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """One row per sequence: q, k, v, out [B, H, D]; the state fp32 [B, H, D, D] is updated in place unless new_state is given.
     scale: 1 / sqrt(D) if not given."""
-    B, H, D = q.shape
     new_state = state if new_state is None else new_state
+    if out is None and (made := _native("linear_step", q, k, v, log_decay, state, q.shape[-1] ** -0.5 if scale is None else scale, new_state)) is not None:
+        return made, new_state
+    B, H, D = q.shape
     _check_linear(q, k, v, log_decay, B, state, new_state)
     assert out is None or (out.shape == q.shape and out.dtype == q.dtype)
     with _on_device_of(q, k, v, log_decay, state, out, new_state):
@@ -512,9 +520,9 @@ def jfa_linear_attention_step(q, k, v, log_decay, state, scale: Optional[float] 
     return out, new_state
 
 
-def _norm_sizes(x, weight, bias, offsets):
-    """(rows, reps, N, B): x [rows, ...] whose last dimensions are weight's (or bias's; without either only the last)."""
-    shape = next((t.shape for t in (weight, bias) if t is not None), x.shape[-1:])
+def _norm_sizes(x, weight, bias, offsets, shape=None):
+    """(rows, reps, N, B): x [rows, ...] whose last dimensions are `shape`, else weight's (or bias's; without either only the last)."""
+    shape = next((t.shape for t in (weight, bias) if t is not None), x.shape[-1:]) if shape is None else shape
     assert x.dim() >= 1 + len(shape) and len(shape) >= 1 and x.shape[x.dim() - len(shape):] == shape, "weight and bias: x's last dimensions"
     assert all(t is None or (t.shape == shape and t.dtype == x.dtype) for t in (weight, bias)), "weight and bias: of one shape, and of x's type"
     N = shape.numel()
@@ -539,7 +547,7 @@ def jfa_layer_norm_backward(x, weight, dy, mean, rstd, offsets=None, dx=None, dw
                             want_dbias: bool = True):
     """dx like x, dweight and dbias of weight's shape (None where not wanted).  normalized_shape: for a layer norm without weight."""
     shape = weight.shape if weight is not None else torch.Size(x.shape[-1:] if normalized_shape is None else normalized_shape)
-    rows, reps, N, B = _norm_sizes(x, torch.empty(shape, dtype=x.dtype, device="meta"), None, offsets)
+    rows, reps, N, B = _norm_sizes(x, weight, None, offsets, shape)
     assert dy.shape == x.shape and dy.dtype == x.dtype and (dx is None or (dx.shape == x.shape and dx.dtype == x.dtype))
     assert all(t.dtype == torch.float32 and t.numel() == rows * reps for t in (mean, rstd)), "mean and rstd: fp32 [rows, reps]"
     assert all(t is None or (t.shape == shape and t.dtype == x.dtype) for t in (weight, dweight, dbias))
