@@ -251,6 +251,7 @@ int jfa_jagged_softmax_backward(const void *y, const void *dy, const int64_t *of
  *   initial_state, final_state, dfinal_state, dinitial_state   fp32 [B, H, D, D], each may be null: an initial state (a gradient of the
  *                        final state) of zeros, a final state (a gradient of the initial state) that is not wanted.  A sample without rows
  *                        hands its state through.
+ *   rows                 rows of the tensors, sum_B or more; with max_len they decide how the work is laid out
  *   workspace            jfa_linear_attention_workspace_bytes(...) bytes of device memory, 16-byte aligned, that nobody else uses until
  *                        the call's work is done; may be null where that is 0 (pass: 0 = forward, 1 = backward)
  *
@@ -259,21 +260,21 @@ int jfa_jagged_softmax_backward(const void *y, const void *dy, const int64_t *of
  * one) is exact to fp32.  A row that is not finite reaches the other rows of its sample and head, earlier ones
  * among them, and nothing else.  The gradient of log_decay is not computed.
  * jfa_linear_attention_step takes one row per sequence, q, k, v, out [B, H, D], and a state [B, H, D, D]; new_state may be `state`.
- * At most JFA_LINEAR_MAX_PAIRS samples times heads.  Everything else as for the calls above.
+ * At most JFA_LINEAR_MAX_PAIRS samples times heads, H * D at most 2^20.  Everything else as for the calls above.
  */
 #define JFA_LINEAR_MAX_PAIRS (1 << 22)
-size_t jfa_linear_attention_workspace_bytes(int64_t B, int64_t max_len, int H, int D, int pass);
-int jfa_linear_attention(const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len, int H,
+size_t jfa_linear_attention_workspace_bytes(int64_t B, int64_t rows, int64_t max_len, int H, int D, int pass);
+int jfa_linear_attention(const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t rows, int64_t max_len, int H,
                          int D, float scale, const float *initial_state, void *out, float *final_state, void *workspace, size_t workspace_bytes,
                          void *stream);
-int jfa_linear_attention_f32(const float *q, const float *k, const float *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len,
+int jfa_linear_attention_f32(const float *q, const float *k, const float *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t rows, int64_t max_len,
                              int H, int D, float scale, const float *initial_state, float *out, float *final_state, void *workspace,
                              size_t workspace_bytes, void *stream);
 int jfa_linear_attention_backward(const void *q, const void *k, const void *v, const void *dout, const float *log_decay, const int64_t *offsets, int64_t B,
-                                  int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state, void *dq, void *dk,
+                                  int64_t rows, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state, void *dq, void *dk,
                                   void *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream);
 int jfa_linear_attention_backward_f32(const float *q, const float *k, const float *v, const float *dout, const float *log_decay, const int64_t *offsets,
-                                      int64_t B, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state,
+                                      int64_t B, int64_t rows, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state,
                                       float *dq, float *dk, float *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream);
 int jfa_linear_attention_step(const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
                               const float *state, void *out, float *new_state, void *stream);

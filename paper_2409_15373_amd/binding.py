@@ -121,8 +121,8 @@ def load() -> ctypes.CDLL:
     lib.jfa_jagged_softmax_backward.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp]
     f32 = ctypes.c_float
     for name, restype, argtypes in (
-            ("jfa_linear_attention", i32, [vp] * 5 + [i64, i64, i32, i32, f32] + [vp] * 4 + [sz, vp]),
-            ("jfa_linear_attention_backward", i32, [vp] * 6 + [i64, i64, i32, i32, f32] + [vp] * 7 + [sz, vp]),
+            ("jfa_linear_attention", i32, [vp] * 5 + [i64, i64, i64, i32, i32, f32] + [vp] * 4 + [sz, vp]),
+            ("jfa_linear_attention_backward", i32, [vp] * 6 + [i64, i64, i64, i32, i32, f32] + [vp] * 7 + [sz, vp]),
             ("jfa_linear_attention_step", i32, [vp] * 4 + [i64, i32, i32, f32] + [vp] * 4),
             ("jfa_layer_norm", i32, [vp] * 4 + [i64] * 4 + [f32] + [vp] * 4),
             ("jfa_layer_norm_backward", i32, [vp] * 6 + [i64] * 4 + [vp] * 4 + [sz, vp]),
@@ -132,7 +132,7 @@ def load() -> ctypes.CDLL:
             getattr(lib, name + suffix).restype = restype
             getattr(lib, name + suffix).argtypes = argtypes
     lib.jfa_linear_attention_workspace_bytes.restype = sz
-    lib.jfa_linear_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32]
+    lib.jfa_linear_attention_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32]
     lib.jfa_layer_norm_workspace_bytes.restype = sz
     lib.jfa_layer_norm_workspace_bytes.argtypes = [i64, i64, i64]
     lib.jfa_embedding_workspace_bytes.restype = sz
@@ -478,9 +478,9 @@ def jfa_linear_attention(q, k, v, log_decay, offsets, max_len: int, scale: Optio
         out = torch.empty_like(q) if out is None else out
         if final_state is None and return_state:
             final_state = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
-        workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, max_len, H, D, 0), q.device)
+        workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, q.shape[0], max_len, H, D, 0), q.device)
         _check(_pick(q.dtype, "jfa_linear_attention")(
-            *(_row_ptr(t, offsets) for t in (q, k, v)), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale, _ptr(initial_state),
+            *(_row_ptr(t, offsets) for t in (q, k, v)), _ptr(log_decay), _ptr(offsets), B, q.shape[0], max_len, H, D, D ** -0.5 if scale is None else scale, _ptr(initial_state),
             _row_ptr(out, offsets),
             _ptr(final_state), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
     return out, final_state
@@ -497,9 +497,9 @@ def jfa_linear_attention_backward(q, k, v, dout, log_decay, offsets, max_len: in
         dq, dk, dv = (torch.empty_like(q) if t is None else t for t in (dq, dk, dv))
         if dinitial_state is None and return_dstate:
             dinitial_state = torch.empty((B, H, D, D), dtype=torch.float32, device=q.device)
-        workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, max_len, H, D, 1), q.device)
+        workspace = _workspace(load().jfa_linear_attention_workspace_bytes(B, q.shape[0], max_len, H, D, 1), q.device)
         _check(_pick(q.dtype, "jfa_linear_attention_backward")(
-            *(_row_ptr(t, offsets) for t in (q, k, v, dout)), _ptr(log_decay), _ptr(offsets), B, max_len, H, D, D ** -0.5 if scale is None else scale,
+            *(_row_ptr(t, offsets) for t in (q, k, v, dout)), _ptr(log_decay), _ptr(offsets), B, q.shape[0], max_len, H, D, D ** -0.5 if scale is None else scale,
             _ptr(initial_state), _ptr(dfinal_state), *(_row_ptr(t, offsets) for t in (dq, dk, dv)), _ptr(dinitial_state), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
     return dq, dk, dv, dinitial_state
 

@@ -808,11 +808,13 @@ int jfa_jagged_softmax_backward(const void *y, const void *dy, const int64_t *of
 // ---- linear attention with a decay for each head ----
 
 namespace {
-int linear_begin(const char *who, int64_t B, int64_t max_len, int H, int D) {
+int linear_begin(const char *who, int64_t B, int64_t rows, int64_t max_len, int H, int D) {
     if (B < 0) return fail(JFA_ERR_INVALID_ARG, "%s: B = %lld is negative", who, (long long)B);
     if (max_len < 0 || max_len >= (int64_t)1 << 31) return fail(JFA_ERR_INVALID_ARG, "%s: bad max_len = %lld", who, (long long)max_len);
+    if (rows < 0) return fail(JFA_ERR_INVALID_ARG, "%s: rows = %lld is negative", who, (long long)rows);
     if (H <= 0) return fail(JFA_ERR_INVALID_ARG, "%s: H = %d must be positive", who, H);
     if (D != 32 && D != 64 && D != 128) return fail(JFA_ERR_UNSUPPORTED, "%s: D = %d is not one of 32, 64, 128", who, D);
+    if ((int64_t)H * D > 1 << 20) return fail(JFA_ERR_UNSUPPORTED, "%s: H * D = %lld exceeds 2^20", who, (long long)H * D);   // 32-bit byte offsets inside a chunk
     if (B > JFA_LINEAR_MAX_PAIRS / H) return fail(JFA_ERR_UNSUPPORTED, "%s: B * H = %lld * %d exceeds %d", who, (long long)B, H, JFA_LINEAR_MAX_PAIRS);
     return JFA_OK;
 }
@@ -825,38 +827,34 @@ int linear_pointers(const char *who, const void *const *tensors, int n, const fl
         if (misaligned(optional[i])) return fail(JFA_ERR_INVALID_ARG, "%s: a state is not 16-byte aligned", who);
     return JFA_OK;
 }
-size_t linear_workspace(int64_t B, int64_t max_len, int H, int D, bool backward, int *segments, int *segment_rows) {
-    *segment_rows = jfa::linear_segment_rows(B, max_len, H, backward ? 3 : 1, jfa::kLinearCus);
-    *segments = max_len > *segment_rows ? (int)((max_len + *segment_rows - 1) / *segment_rows) : 1;
-    return (size_t)((backward ? 2 : 1) * B * H * (*segments - 1)) * D * D * sizeof(float);
-}
 int linear_launch(const char *who, bool f32, const jfa::LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets,
-                  int64_t B, int64_t max_len, int H, int D, void *workspace, size_t workspace_bytes, hipStream_t s) {
-    int segments, segment_rows;
-    const size_t need = linear_workspace(B, max_len, H, D, backward, &segments, &segment_rows);
+                  int64_t B, int64_t rows, int64_t max_len, int H, int D, void *workspace, size_t workspace_bytes, hipStream_t s) {
+    const jfa::LinearPlan plan = jfa::linear_plan(B, rows, max_len, H, D, backward);
+    const size_t need = (size_t)plan.bytes;
     if (workspace_bytes < need || (need && !workspace))
         return fail(JFA_ERR_INVALID_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : 0, need);
     if (need && misaligned(workspace)) return fail(JFA_ERR_INVALID_ARG, "%s: the workspace is not 16-byte aligned", who);
+    if (B * H * plan.segments >= (int64_t)1 << 24) return fail(JFA_ERR_UNSUPPORTED, "%s: B = %lld samples of up to %lld rows are too many", who, (long long)B, (long long)max_len);
     ScopedTimer tm(backward ? "linear_attention_bwd" : "linear_attention", s);
-    const hipError_t e = jfa::launch_linear_walks(f32, walks, backward, states, log_decay, offsets, B, H, D, segments, segment_rows, (float *)workspace, s);
+    const hipError_t e = jfa::launch_linear_walks(f32, walks, backward, states, log_decay, offsets, B, H, D, plan, workspace, s);
     return e == hipSuccess ? JFA_OK : hip_fail("linear attention kernel", e);
 }
-int linear_forward(const char *who, bool f32, const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B,
+int linear_forward(const char *who, bool f32, const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t rows,
                    int64_t max_len, int H, int D, float scale, const float *initial_state, void *out, float *final_state, void *workspace,
                    size_t workspace_bytes, hipStream_t s) {
-    int st = linear_begin(who, B, max_len, H, D);
+    int st = linear_begin(who, B, rows, max_len, H, D);
     if (st != JFA_OK || B == 0) return st;
     const void *tensors[] = {q, k, v, out, offsets, log_decay};
     const float *states[] = {initial_state, final_state};
     if ((st = linear_pointers(who, tensors, 6, states, 2)) != JFA_OK) return st;
     const jfa::LinearWalks walks{{{q, k, v, out, initial_state, final_state, 1.0f, scale, false, false, false, 0}}};
-    return linear_launch(who, f32, walks, false, final_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
+    return linear_launch(who, f32, walks, false, final_state != nullptr, log_decay, offsets, B, rows, max_len, H, D, workspace, workspace_bytes, s);
 }
 int linear_backward(const char *who, bool f32, const void *q, const void *k, const void *v, const void *dout, const float *log_decay,
-                    const int64_t *offsets, int64_t B, int64_t max_len, int H, int D, float scale, const float *initial_state,
+                    const int64_t *offsets, int64_t B, int64_t rows, int64_t max_len, int H, int D, float scale, const float *initial_state,
                     const float *dfinal_state, void *dq, void *dk, void *dv, float *dinitial_state, void *workspace, size_t workspace_bytes,
                     hipStream_t s) {
-    int st = linear_begin(who, B, max_len, H, D);
+    int st = linear_begin(who, B, rows, max_len, H, D);
     if (st != JFA_OK || B == 0) return st;
     const void *tensors[] = {q, k, v, dout, dq, dk, dv, offsets, log_decay};
     const float *states[] = {initial_state, dfinal_state, dinitial_state};
@@ -864,11 +862,11 @@ int linear_backward(const char *who, bool f32, const void *q, const void *k, con
     const jfa::LinearWalks walks{{{dout, v, k, dq, initial_state, nullptr, 1.0f, scale, false, true, false, 0},
                                   {v, dout, q, dk, dfinal_state, nullptr, scale, 1.0f, true, true, true, 1},   // the two have one state
                                   {k, q, dout, dv, dfinal_state, dinitial_state, scale, 1.0f, true, false, false, 1}}};
-    return linear_launch(who, f32, walks, true, dinitial_state != nullptr, log_decay, offsets, B, max_len, H, D, workspace, workspace_bytes, s);
+    return linear_launch(who, f32, walks, true, dinitial_state != nullptr, log_decay, offsets, B, rows, max_len, H, D, workspace, workspace_bytes, s);
 }
 int linear_step(const char *who, bool f32, const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
                 const float *state, void *out, float *new_state, hipStream_t s) {
-    int st = linear_begin(who, B, 1, H, D);
+    int st = linear_begin(who, B, B, 1, H, D);
     if (st != JFA_OK || B == 0) return st;
     const void *tensors[] = {q, k, v, out, state, new_state, log_decay};
     if ((st = linear_pointers(who, tensors, 7, nullptr, 0)) != JFA_OK) return st;
@@ -878,33 +876,32 @@ int linear_step(const char *who, bool f32, const void *q, const void *k, const v
 }
 }  // namespace
 
-size_t jfa_linear_attention_workspace_bytes(int64_t B, int64_t max_len, int H, int D, int pass) {
-    if (linear_begin("jfa_linear_attention_workspace_bytes", B, max_len, H, D) != JFA_OK || B == 0) return 0;
-    int segments, segment_rows;
-    return linear_workspace(B, max_len, H, D, pass != 0, &segments, &segment_rows);
+size_t jfa_linear_attention_workspace_bytes(int64_t B, int64_t rows, int64_t max_len, int H, int D, int pass) {
+    if (linear_begin("jfa_linear_attention_workspace_bytes", B, rows, max_len, H, D) != JFA_OK || B == 0) return 0;
+    return (size_t)jfa::linear_plan(B, rows, max_len, H, D, pass != 0).bytes;
 }
-int jfa_linear_attention(const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len, int H,
+int jfa_linear_attention(const void *q, const void *k, const void *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t rows, int64_t max_len, int H,
                          int D, float scale, const float *initial_state, void *out, float *final_state, void *workspace, size_t workspace_bytes,
                          void *stream) {
-    return linear_forward("jfa_linear_attention", false, q, k, v, log_decay, offsets, B, max_len, H, D, scale, initial_state, out, final_state, workspace,
+    return linear_forward("jfa_linear_attention", false, q, k, v, log_decay, offsets, B, rows, max_len, H, D, scale, initial_state, out, final_state, workspace,
                           workspace_bytes, (hipStream_t)stream);
 }
-int jfa_linear_attention_f32(const float *q, const float *k, const float *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t max_len,
+int jfa_linear_attention_f32(const float *q, const float *k, const float *v, const float *log_decay, const int64_t *offsets, int64_t B, int64_t rows, int64_t max_len,
                              int H, int D, float scale, const float *initial_state, float *out, float *final_state, void *workspace,
                              size_t workspace_bytes, void *stream) {
-    return linear_forward("jfa_linear_attention_f32", true, q, k, v, log_decay, offsets, B, max_len, H, D, scale, initial_state, out, final_state, workspace,
+    return linear_forward("jfa_linear_attention_f32", true, q, k, v, log_decay, offsets, B, rows, max_len, H, D, scale, initial_state, out, final_state, workspace,
                           workspace_bytes, (hipStream_t)stream);
 }
 int jfa_linear_attention_backward(const void *q, const void *k, const void *v, const void *dout, const float *log_decay, const int64_t *offsets, int64_t B,
-                                  int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state, void *dq, void *dk,
+                                  int64_t rows, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state, void *dq, void *dk,
                                   void *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream) {
-    return linear_backward("jfa_linear_attention_backward", false, q, k, v, dout, log_decay, offsets, B, max_len, H, D, scale, initial_state, dfinal_state, dq,
+    return linear_backward("jfa_linear_attention_backward", false, q, k, v, dout, log_decay, offsets, B, rows, max_len, H, D, scale, initial_state, dfinal_state, dq,
                            dk, dv, dinitial_state, workspace, workspace_bytes, (hipStream_t)stream);
 }
 int jfa_linear_attention_backward_f32(const float *q, const float *k, const float *v, const float *dout, const float *log_decay, const int64_t *offsets,
-                                      int64_t B, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state,
+                                      int64_t B, int64_t rows, int64_t max_len, int H, int D, float scale, const float *initial_state, const float *dfinal_state,
                                       float *dq, float *dk, float *dv, float *dinitial_state, void *workspace, size_t workspace_bytes, void *stream) {
-    return linear_backward("jfa_linear_attention_backward_f32", true, q, k, v, dout, log_decay, offsets, B, max_len, H, D, scale, initial_state, dfinal_state,
+    return linear_backward("jfa_linear_attention_backward_f32", true, q, k, v, dout, log_decay, offsets, B, rows, max_len, H, D, scale, initial_state, dfinal_state,
                            dq, dk, dv, dinitial_state, workspace, workspace_bytes, (hipStream_t)stream);
 }
 int jfa_linear_attention_step(const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,

@@ -39,12 +39,12 @@ using Product = int (*)(const void *, const void *, const int64_t *, int64_t, in
 using Softmax = int (*)(const void *, const int64_t *, int64_t, int64_t, int, void *, void *);
 using SoftmaxBackward = int (*)(const void *, const void *, const int64_t *, int64_t, int64_t, int, void *, void *);
 
-using Linear = int (*)(const void *, const void *, const void *, const float *, const int64_t *, int64_t, int64_t, int, int, float, const float *, void *,
+using Linear = int (*)(const void *, const void *, const void *, const float *, const int64_t *, int64_t, int64_t, int64_t, int, int, float, const float *, void *,
                        float *, void *, size_t, void *);
-using LinearBackward = int (*)(const void *, const void *, const void *, const void *, const float *, const int64_t *, int64_t, int64_t, int, int, float,
+using LinearBackward = int (*)(const void *, const void *, const void *, const void *, const float *, const int64_t *, int64_t, int64_t, int64_t, int, int, float,
                                const float *, const float *, void *, void *, void *, float *, void *, size_t, void *);
 using LinearStep = int (*)(const void *, const void *, const void *, const float *, int64_t, int, int, float, const float *, void *, float *, void *);
-using LinearWorkspace = size_t (*)(int64_t, int64_t, int, int, int);
+using LinearWorkspace = size_t (*)(int64_t, int64_t, int64_t, int, int, int);
 using Norm = int (*)(const void *, const void *, const void *, const int64_t *, int64_t, int64_t, int64_t, int64_t, float, void *, float *, float *, void *);
 using NormBackward = int (*)(const void *, const void *, const void *, const float *, const float *, const int64_t *, int64_t, int64_t, int64_t, int64_t, void *,
                              void *, void *, void *, size_t, void *);
@@ -434,9 +434,9 @@ std::pair<Tensor, Tensor> linear_call(const Tensor &q, const Tensor &k, const Te
     const int64_t B = offsets.numel() - 1;
     const Tensor out = at::empty(q.sizes(), q.options());
     const Tensor final_state = want_state ? at::empty({B, H, D, D}, q.options().dtype(at::kFloat)) : Tensor();
-    const size_t need = lib.linear_workspace(B, max_len, H, D, 0);
+    const size_t need = lib.linear_workspace(B, q.size(0), max_len, H, D, 0);
     const Tensor workspace = bytes(need, q);
-    check_call(lib.linear[kind(q)](q.data_ptr(), k.data_ptr(), v.data_ptr(), floats(log_decay), longs(offsets), B, max_len, H, D, (float)scale, floats_or_null(initial),
+    check_call(lib.linear[kind(q)](q.data_ptr(), k.data_ptr(), v.data_ptr(), floats(log_decay), longs(offsets), B, q.size(0), max_len, H, D, (float)scale, floats_or_null(initial),
                                    out.data_ptr(), static_cast<float *>(place(final_state)), place(workspace), need, stream()), false);
     return {out, final_state};
 }
@@ -471,9 +471,9 @@ struct LinearAttention : torch::autograd::Function<LinearAttention> {
         if (dfinal.defined()) check_back(dfinal, {B, H, D, D}, at::kFloat, device);
         const Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(q.sizes(), q.options()), dv = at::empty(q.sizes(), q.options());
         const Tensor dinitial = call[6] ? at::empty({B, H, D, D}, q.options().dtype(at::kFloat)) : Tensor();
-        const size_t need = lib.linear_workspace(B, max_len, H, D, 1);
+        const size_t need = lib.linear_workspace(B, q.size(0), max_len, H, D, 1);
         const Tensor workspace = bytes(need, q);
-        check_call(lib.linear_backward[type == at::kFloat](q.data_ptr(), k.data_ptr(), v.data_ptr(), dout.data_ptr(), floats(log_decay), longs(offsets), B, max_len, H, D,
+        check_call(lib.linear_backward[type == at::kFloat](q.data_ptr(), k.data_ptr(), v.data_ptr(), dout.data_ptr(), floats(log_decay), longs(offsets), B, q.size(0), max_len, H, D,
                                                            (float)ctx->saved_data["scale"].toDouble(), static_cast<float *>(place(saved[5])), static_cast<float *>(place(dfinal)),
                                                            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), static_cast<float *>(place(dinitial)), place(workspace), need, stream()),
                    true);

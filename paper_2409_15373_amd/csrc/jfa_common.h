@@ -833,10 +833,16 @@ struct LinearWalk {
     int carried;             // which of those between segments are this walk's
 };
 struct LinearWalks { LinearWalk walk[3]; };
-constexpr int kLinearCus = 256;   // compute units: the workspace's size follows from the sizes alone
-int linear_segment_rows(int64_t B, int64_t max_len, int H, int walks, int cus);
+struct LinearPlan {
+    int segments;            // at most, of a sample
+    int64_t segment_rows;
+    int between;             // states between segments, for each walk and head
+    bool ordered;            // longest samples first
+    int64_t order_words, bytes;   // of the workspace: the order, all of it
+};
+LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, bool backward);
 hipError_t launch_linear_walks(bool f32, const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
-                               int D, int segments, int segment_rows, float *carried, hipStream_t stream);
+                               int D, const LinearPlan &p, void *workspace, hipStream_t stream);
 hipError_t launch_linear_step(bool f32, const void *q, const void *k, const void *v, const float *log_decay, int64_t B, int H, int D, float scale,
                               const float *state, void *out, float *new_state, hipStream_t stream);
 

@@ -120,6 +120,10 @@ template <int left> constexpr int vmem_left() { return (left & 15) | ((left >> 4
 constexpr int kNoVmem = vmem_left<0>();
 __device__ inline float power(float log2_g, int n) { return fast_exp2(log2_g * (float)n); }   // n >= 0
 
+// Where the states between a sample's segments start, in states: a sample that begins in row r has at most as many as there are multiples of
+// segment_rows in its rows, so the r / segment_rows-th is its first, `between` of them in all for each walk and head.
+__device__ inline int64_t state_between(int walk, int h, int H, int between, int64_t first, int segment_rows) { return ((int64_t)walk * H + h) * between + first / segment_rows; }
+
 }  // namespace
 
 // A workgroup takes one (sample, head, segment), blockIdx.x, through ROLES walks that go the same way over the same tensors: one of them (walk
@@ -131,17 +135,22 @@ __device__ inline float power(float log2_g, int n) { return fast_exp2(log2_g * (
 // kStateOnly: the state that a segment adds to, for those with a segment after them, into `carried`.
 template <typename T, int D, int ROLES, int kParts, bool kStateOnly>
 __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
-                                                                       int H, int segments, int segment_rows, float *__restrict__ carried) {
+                                                                       const int32_t *__restrict__ order, int B, int H, int segments, int segment_rows, int between,
+                                                                       float *__restrict__ carried) {
     typedef Elem<T> E;
     typedef typename E::Operand Operand;
     constexpr int kRows = E::kRows, kSize = (int)sizeof(T), kStateTiles = D / 32, kSteps = D / 16, kSplit = E::kSplit, kWaves = kStateTiles * ROLES;
     constexpr int kTiles = kRows / 32, kPTiles = kTiles * (kTiles + 1) / 2;
     constexpr int kChunks = D * kSize / 16, kTileBytes = kRows * kChunks * 16, kLoads = kRows * kChunks / (64 * kWaves);   // 16-byte chunks of a row; copies of a tile per wave
-    // Places of tiles.  Two walks: two of each tile, the next chunk's are on their way while this one's are in use.  One walk: two workgroups of a
-    // compute unit have room for four tiles each: A, C and two of B; the next B is fetched from the start of a chunk on, the next A once the state's
-    // product with A is done, the next C once the chunk is, which is in time for the products with C of the next chunk.
-    constexpr int kPlaces = ROLES == 2 ? 8 : 4;
-    __shared__ __attribute__((aligned(16))) char lds[kPlaces * kTileBytes];
+    // Places of tiles.  A is free for the next chunk's once the state's product with it is done, in the middle of a chunk.  B and, of two walks, C (their B
+    // and C change places) are read to the end: there are two of each, the next chunk's fetched from the start of a chunk on.  One walk's C is fetched when the
+    // chunk before is done, which is in time for the products with it.  So two workgroups have room on a compute unit (D = 128, two walks: one).
+    constexpr int kPlaces = ROLES == 2 ? 6 : 4;
+    // P: its tiles are shared out among a walk's waves, which leave them as operands, 16 bytes per lane; a single wave (and the fp32 kernels, whose P is
+    // one tile) has it in registers.
+    constexpr bool kShareP = !kStateOnly && kPTiles > 1 && kStateTiles > 1;
+    constexpr int kPBytes = kShareP ? kPTiles * 2 * kSplit * 1024 : 0;
+    __shared__ __attribute__((aligned(16))) char lds[kPlaces * kTileBytes + ROLES * kPBytes];
     __shared__ float powers[ROLES][2][2 * kRows];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -149,18 +158,23 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
     const int col = lane & 31, half = lane >> 5;
     const int which = ROLES == 2 ? 1 : (int)blockIdx.y;   // the first role's walk
     const LinearWalk &walk = walks.walk[which + role];
-    const int pair = blockIdx.x / segments, segment = blockIdx.x - pair * segments;
-    const int b = pair / H, h = pair - b * H;
+    // Workgroups go to the eight dies in turn.  Heads that share 128-byte lines are for one of them, whose L2 reads a line once (600 rows x 512 x 4, D = 32: 103 -> 67 us).
+    constexpr bool kSameDie = D * sizeof(T) < 128;
+    const int at = kSameDie ? (int)(blockIdx.x / (8 * H)) * 8 + (int)(blockIdx.x % 8) : (int)(blockIdx.x / H), h = kSameDie ? (int)(blockIdx.x / 8) % H : (int)(blockIdx.x % H);
+    const int at_sample = at / segments, segment = at - at_sample * segments;
+    if (kSameDie && at_sample >= B) return;
+    const int b = order ? order[at_sample] : at_sample, pair = b * H + h;
     const int64_t first = offsets[b];
     const int64_t L = offsets[b + 1] - first;
     const int64_t t0 = (int64_t)segment * segment_rows;   // rows are counted in the order of the walk
     const bool last = t0 + segment_rows >= L;
     if (kStateOnly ? last || segment == segments - 1 : (t0 >= L && segment > 0)) return;
+    if (segments > 1 && first / segment_rows + segment > between) return;   // (more rows than the caller said there were)
     const int64_t left = L - t0;
     const int n = (int)(left < segment_rows ? left : segment_rows);   // rows of this segment; 0 for an empty sample
     const bool reverse = walk.reverse;
     const float lg = log2_decay(log_decay[h]);
-    float *const passed = carried + ((int64_t)walk.carried * (gridDim.x / segments) + pair) * (segments - 1) * D * D;
+    float *const passed = carried + state_between(walk.carried, h, H, between, first, segment_rows) * D * D;
     float *const state_out = kStateOnly ? passed + (int64_t)segment * D * D : last && walk.state_out ? walk.state_out + (int64_t)pair * D * D : nullptr;
 
     f32x16 S[kStateTiles];   // tile m: rows 32 m .. (dimension of B), columns 32 strip .. (dimension of C)
@@ -190,12 +204,22 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
     const T *const a0 = (const T *)walks.walk[which].a, *const a1 = (const T *)walks.walk[ROLES == 2 ? 2 : which].a;
     const T *const b0 = (const T *)walks.walk[which].b, *const c0 = (const T *)walks.walk[which].c;
     // The rows from `rows` on are not there: the last one takes their place.  Whatever it is, P's mask and the decayed rows' zeros keep it out.
+    auto offset_of = [&](int u, int rows) {
+        const int at = (u * kWaves + wave) * 64 + lane, t = at / kChunks, c = at % kChunks ^ swizzle<kChunks>(t), there = t < rows ? t : rows - 1;
+        return (uint32_t)(reverse ? kRows - 1 - there : there) * row_bytes + c * 16;
+    };
+    uint32_t offsets_of_all[kLoads];   // of a whole chunk
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) offsets_of_all[u] = offset_of(u, kRows);
     auto copy = [&](const T *tensor, int64_t from, int rows, int place) {
         const T *const base = reinterpret_cast<const T *>(uniform64((int64_t)(tensor + from)));
+        char *const dst = lds + place * kTileBytes + wave * 1024;
+        if (rows >= kRows) {
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int at = (u * kWaves + wave) * 64 + lane, t = at / kChunks, c = at % kChunks ^ swizzle<kChunks>(t), there = t < rows ? t : rows - 1;
-            bd_dma16(base, (uint32_t)(reverse ? kRows - 1 - there : there) * row_bytes + c * 16, lds + place * kTileBytes + (u * kWaves + wave) * 1024);
+            for (int u = 0; u < kLoads; ++u) bd_dma16(base, offsets_of_all[u], dst + u * kWaves * 1024);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) bd_dma16(base, offset_of(u, rows), dst + u * kWaves * 1024);
         }
     };
     const int row_base = E::template rows_base<D>(lane), col_base = E::template cols_base<D, false>(lane) ^ (strip * 32 * kSize), col_base_b = E::template cols_base<D, true>(lane);
@@ -217,7 +241,7 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
             copy(a0, low, n, 0);
             copy(a1, low, n, 1);
             copy(b0, low, n, 2);
-            copy(c0, low, n, 3);
+            copy(c0, low, n, 4);
         } else {
             copy(b0, low, n, 2);
             if (!kStateOnly) copy(a0, low, n, 0);
@@ -230,25 +254,24 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
         __syncthreads();   // the tiles fetched so far are there, and the last chunk's are free
         if constexpr (ROLES == 2) {
             if (more) {
-                copy(a0, low + low_step, n - r0 - kRows, 4 * (turn ^ 1));
-                copy(a1, low + low_step, n - r0 - kRows, 4 * (turn ^ 1) + 1);
-                copy(b0, low + low_step, n - r0 - kRows, 4 * (turn ^ 1) + 2);
-                copy(c0, low + low_step, n - r0 - kRows, 4 * (turn ^ 1) + 3);
+                copy(b0, low + low_step, n - r0 - kRows, 2 + (turn ^ 1));
+                copy(c0, low + low_step, n - r0 - kRows, 4 + (turn ^ 1));
             }
         } else {
             copy(c0, low, n - r0, 1);
             if (more) copy(b0, low + low_step, n - r0 - kRows, 2 + (turn ^ 1));
         }
-        // (C waits for its copies, at most the next B's later: stores have been waited for above)
+        // One walk's C: its copies are the ones in front of the next B's.  (Stores have been waited for above.)
         auto c_is_there = [&]() {
             if constexpr (ROLES == 1) {
                 if (more) __builtin_amdgcn_s_waitcnt(vmem_left<kLoads>());
                 else __builtin_amdgcn_s_waitcnt(kNoVmem);
-                __syncthreads();
             }
+            __syncthreads();   // P is there, too, and A is free
         };
-        const char *const at = lds + (ROLES == 2 ? 4 * turn + role : 0) * kTileBytes;
-        const char *const bt = lds + (ROLES == 2 ? 4 * turn + 2 + role : 2 + turn) * kTileBytes, *const ct = lds + (ROLES == 2 ? 4 * turn + 3 - role : 1) * kTileBytes;
+        const char *const at = lds + role * kTileBytes;
+        const char *const bt = lds + (ROLES == 2 ? 2 + 2 * role + turn : 2 + turn) * kTileBytes, *const ct = lds + (ROLES == 2 ? 4 - 2 * role + turn : 1) * kTileBytes;
+        char *const pt = lds + kPlaces * kTileBytes + role * kPBytes;
         Operand c[2 * kTiles];   // the chunk's rows of C, this wave's columns
         if (kStateOnly) {
             c_is_there();
@@ -256,15 +279,54 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
             for (int k = 0; k < 2 * kTiles; ++k) c[k] = E::template cols<D>(ct, col_base, 0, k * 16);
         }
         if (!kStateOnly) {
-            // P^T, tiles (rows j of B) x (columns i of A), zero above the diagonal: every wave has all of it, as operands
-            Operand P[kPTiles][2][kSplit];
-            {
+            // P^T, tiles (rows j of B) x (columns i of A), zero above the diagonal
+            Operand P[kShareP ? 1 : kPTiles][2][kSplit];
+            const float *const near = my_powers[0] + kRows + col - 4 * half;   // [-(8 g + e)]: g^(i - j)
+            auto weighted = [&](f32x16 &p, int t, auto &&put) {   // t: 0, 2 on the diagonal, 1 below it; put(contraction step, part, operand)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float weight = near[(t == 1 ? 32 : 0) - ((v >> 2) * 8 + (v & 3))];
+                    p[v] = t != 1 && col < acc_row(v, half) ? 0.0f : p[v] * weight;
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    f32x8 x = eight(p, k * 8);
+#pragma unroll
+                    for (int part = 0; part < kSplit; ++part) {
+                        const Operand y = E::pack(x);
+                        put(k, part, y);
+                        if (part + 1 < kSplit) x -= E::widen(y);
+                    }
+                }
+            };
+            if constexpr (kShareP) {
+#pragma unroll
+                for (int t = 0; t < kPTiles; ++t) {
+                    if (t % kStateTiles != strip) continue;
+                    // operands one step ahead of the products that use them: left alone, every read sits right in front of its product
+                    Operand a[2], x[2];
+                    auto read = [&](int ks) {
+                        a[ks & 1] = E::template rows<D>(at, row_base, t > 0 ? 32 : 0, ks * 16);
+                        x[ks & 1] = E::template rows<D>(bt, row_base, t > 1 ? 32 : 0, ks * 16);
+                    };
+                    f32x16 p;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) p[v] = 0.0f;
+                    read(0);
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks) {
+                        if (ks + 1 < kSteps) read(ks + 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                        p = E::product(x[ks & 1], a[ks & 1], p);
+                    }
+                    weighted(p, t, [&](int k, int part, const Operand &y) { *reinterpret_cast<Operand *>(pt + ((t * 2 + k) * kSplit + part) * 1024 + lane * 16) = y; });
+                }
+            } else {
                 f32x16 p[kPTiles];
 #pragma unroll
                 for (int t = 0; t < kPTiles; ++t)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) p[t][v] = 0.0f;
-                // operands one step ahead of the products that use them: left alone, every read sits right in front of its product
                 Operand a[2][kTiles], x[2][kTiles];
                 auto read = [&](int ks) {
 #pragma unroll
@@ -284,24 +346,8 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
                         p[2] = E::product(x[ks & 1][1], a[ks & 1][1], p[2]);
                     }
                 }
-                const float *const near = my_powers[0] + kRows + col - 4 * half;   // [-(8 g + e)]: g^(i - j)
 #pragma unroll
-                for (int t = 0; t < kPTiles; ++t) {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const float weight = near[(t == 1 ? 32 : 0) - ((v >> 2) * 8 + (v & 3))];
-                        p[t][v] = t != 1 && col < acc_row(v, half) ? 0.0f : p[t][v] * weight;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        f32x8 x = eight(p[t], k * 8);
-#pragma unroll
-                        for (int part = 0; part < kSplit; ++part) {
-                            P[t][k][part] = E::pack(x);
-                            if (part + 1 < kSplit) x -= E::widen(P[t][k][part]);
-                        }
-                    }
-                }
+                for (int t = 0; t < kPTiles; ++t) weighted(p[t], t, [&](int k, int part, const Operand &y) { P[t][k][part] = y; });
             }
             asm volatile("" ::: "memory");   // A's operands are read again: kept from above they would cost 64 registers
             // out^T = C^T P^T + g^(i + 1) S^T A^T, this wave's columns of C
@@ -329,8 +375,11 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
                     if (part + 1 < kSplit) x -= E::widen(y);
                 }
             }
-            c_is_there();   // and A is free
-            if (ROLES == 1 && more) copy(a0, low + low_step, n - r0 - kRows, 0);
+            c_is_there();
+            if (more) {
+                copy(a0, low + low_step, n - r0 - kRows, 0);
+                if constexpr (ROLES == 2) copy(a1, low + low_step, n - r0 - kRows, 1);
+            }
 #pragma unroll
             for (int k = 0; k < 2 * kTiles; ++k) c[k] = E::template cols<D>(ct, col_base, 0, k * 16);
 #pragma unroll
@@ -341,8 +390,12 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
             for (int ks = 0; ks < 2 * kTiles; ++ks)
 #pragma unroll
                 for (int part = 0; part < kSplit; ++part) {
-                    if (ks < 2) o[0] = E::product(c[ks], P[0][ks & 1][part], o[0]);
-                    if constexpr (kTiles == 2) o[1] = E::product(c[ks], P[ks < 2 ? 1 : 2][ks & 1][part], o[1]);
+                    const auto p = [&](int t) -> Operand {
+                        if constexpr (kShareP) return *reinterpret_cast<const Operand *>(pt + ((t * 2 + (ks & 1)) * kSplit + part) * 1024 + lane * 16);
+                        else return P[t][ks & 1][part];
+                    };
+                    if (ks < 2) o[0] = E::product(c[ks], p(0), o[0]);
+                    if constexpr (kTiles == 2) o[1] = E::product(c[ks], p(ks < 2 ? 1 : 2), o[1]);
                 }
             char *const out = reinterpret_cast<char *>((T *)walk.out + low);
 #pragma unroll
@@ -405,14 +458,16 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
 
 // carried[m] (what segment m adds) -> the state in front of segment m + 1, for every (walk, sample, head) and element.
 __global__ __launch_bounds__(256) void linear_carry_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
-                                                           int H, int D, int segments, int segment_rows, float *__restrict__ carried) {
+                                                           int H, int D, int segments, int segment_rows, int between, float *__restrict__ carried) {
     const int blocks = D * D / 1024;   // 1024 elements, four per thread, per workgroup
     const int pair = blockIdx.x / blocks, at = (blockIdx.x - pair * blocks) * 1024 + threadIdx.x * 4;
     const LinearWalk &walk = walks.walk[blockIdx.y];
     const int b = pair / H;
     const int64_t L = offsets[b + 1] - offsets[b];
-    const int64_t passed = (L + segment_rows - 1) / segment_rows - 1;   // segments with one after them
-    const int n = (int)(passed < segments - 1 ? passed : segments - 1);
+    const int64_t first = offsets[b], room = between - first / segment_rows;
+    int64_t n = (L + segment_rows - 1) / segment_rows - 1;   // segments with one after them
+    n = n < segments - 1 ? n : segments - 1;
+    n = n < room ? n : room;
     if (n <= 0) return;
     const float decay = fast_exp2(log2_decay(log_decay[pair - b * H]) * (float)segment_rows);
     f32x4 S = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -422,10 +477,10 @@ __global__ __launch_bounds__(256) void linear_carry_kernel(LinearWalks walks, co
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[e] = from[walk.transposed ? (c + e) * D + r : at + e];
     }
-    f32x4 *x = reinterpret_cast<f32x4 *>(carried + ((int64_t)walk.carried * (gridDim.x / blocks) + pair) * (segments - 1) * D * D + at);
+    f32x4 *x = reinterpret_cast<f32x4 *>(carried + state_between(walk.carried, pair - b * H, H, between, first, segment_rows) * D * D + at);
     const int64_t stride = (int64_t)D * D / 4;
-    constexpr int kAhead = 8;
-    for (int m0 = 0; m0 < n; m0 += kAhead) {
+    constexpr int kAhead = 32;   // states on their way at a time: a trip to memory for each 8 of them took 15 us for 63 (16 walks)
+    for (int64_t m0 = 0; m0 < n; m0 += kAhead) {
         f32x4 y[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
@@ -470,56 +525,85 @@ __global__ __launch_bounds__(256) void linear_step_kernel(const T *__restrict__ 
     if (r0 == 0) Elem<T>::store4(out + row + strip * kCols + g * 4, sums[tid] * scale);
 }
 
-// Rows of a segment: so many that every compute unit has two walks, at least kLeastSegment, and always whole chunks.
-int linear_segment_rows(int64_t B, int64_t max_len, int H, int walks, int cus) {
-    constexpr int64_t kLeastSegment = 256;
-    const int64_t pairs = B * H * walks, wanted = (2 * (int64_t)cus + pairs - 1) / pairs;   // segments per pair
-    int64_t rows = (max_len + wanted - 1) / wanted;
-    rows = (rows + 63) / 64 * 64;
-    if (rows < kLeastSegment) rows = kLeastSegment;
-    if (rows >= max_len) rows = (max_len + 63) / 64 * 64;
-    return (int)(rows > 0 ? rows : 64);
+// How a call is laid out.  A walk goes a chunk of 64 rows at a time, 3.5 us each (bf16, D = 128) where it has a compute unit to itself and 7 where two walks
+// share it, by when the two have 4.5 TB/s of the memory.  So what takes longest is either all rows, W = rows * H / (2 * 256) of them for each place, or one
+// long sample's walk.  A sample longer than that is cut into segments: a pass over k and v for the state that each of them adds, a scan, and the
+// walks of all segments at once, at about 1.65 times W.  It pays where half the longest sample (alone on its compute unit at last) is longer than that and
+// the two passes over a segment.  8 x 2 samples of up to 16000 rows (D = 128) otherwise: 250 chunks one after the other.
+// Many samples of different lengths that are not cut are walked longest first: the walks that are left at the end are short ones (512 x 4 samples of up to 1024
+// rows, forward 307 -> 260 us); the order is made by the attention's scheduler.
+LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, bool backward) {
+    constexpr int64_t kPlaces = 2 * 256, kLeastSegment = 256, kMostSegment = 1024;
+    LinearPlan p;
+    const int64_t W = (int64_t)((double)rows * H / kPlaces);
+    p.segments = 1;
+    p.segment_rows = max_len;
+    p.between = 0;
+    if (max_len > rows) max_len = rows;
+    if (max_len > 640 + 3.3 * W) {
+        int64_t segment = (W + 63) / 64 * 64;
+        segment = segment < kLeastSegment ? kLeastSegment : segment > kMostSegment ? kMostSegment : segment;
+        if (segment < max_len) {
+            p.segments = (int)((max_len + segment - 1) / segment);
+            p.segment_rows = segment;
+            p.between = (int)(rows / segment);
+        }
+    }
+    p.ordered = p.segments == 1 && B > 1 && B * H > kPlaces && max_len >= 512 && (double)max_len * B > 1.2 * rows;
+    p.order_words = p.ordered ? (2 * B + 1 + kNumCounters + 63) / 64 * 64 : 0;
+    p.bytes = p.order_words * 4 + (int64_t)(backward ? 2 : 1) * H * p.between * D * D * 4;
+    return p;
 }
 
 template <typename T, int D, int kParts>
-static void launch_walks(const LinearWalks &walks, bool backward, const float *log_decay, const int64_t *offsets, int64_t B, int H, int segments, int segment_rows,
-                         float *carried, hipStream_t stream) {
-    const unsigned blocks = (unsigned)(B * H * segments);
+static void launch_walks(const LinearWalks &walks, bool backward, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H, int segments,
+                         int segment_rows, int between, float *carried, hipStream_t stream) {
+    const unsigned blocks = (unsigned)((D * sizeof(T) < 128 ? (B * segments + 7) / 8 * 8 : B * segments) * H);
     if (segments > 1) {   // walk 0, and of the two that go back, which have one state, walk 2
         const LinearWalks states{{walks.walk[0], walks.walk[2], walks.walk[2]}};
         const int n = backward ? 2 : 1;
-        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, true>), dim3(blocks, n), dim3(2 * D), 0, stream, states, log_decay, offsets, H, segments, segment_rows, carried);
+        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, true>), dim3(blocks, n), dim3(2 * D), 0, stream, states, log_decay, offsets, order, (int)B, H, segments, segment_rows, between, carried);
         hipLaunchKernelGGL(linear_carry_kernel, dim3((unsigned)(B * H * (D * D / 1024)), n), dim3(256), 0, stream, states, log_decay, offsets, H, D, segments, segment_rows,
-                           carried);
+                           between, carried);
     }
-    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, false>), dim3(blocks), dim3(2 * D), 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
+    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, false>), dim3(blocks), dim3(2 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows, between, carried);
     if (backward)
-        hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, H, segments, segment_rows, carried);
+        hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows, between, carried);
 }
 template <typename T, int D>
-static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H, int segments,
-                               int segment_rows, float *carried, hipStream_t stream) {
-    if constexpr (sizeof(T) == 4) launch_walks<T, D, 1>(walks, backward, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
-    else if (states) launch_walks<T, D, 3>(walks, backward, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
-    else launch_walks<T, D, 2>(walks, backward, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
+static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H,
+                               const LinearPlan &p, float *carried, hipStream_t stream) {
+    const int segment_rows = (int)p.segment_rows;
+    if constexpr (sizeof(T) == 4) launch_walks<T, D, 1>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, carried, stream);
+    else if (states) launch_walks<T, D, 3>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, carried, stream);
+    else launch_walks<T, D, 2>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, carried, stream);
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H, int D,
-                               int segments, int segment_rows, float *carried, hipStream_t stream) {
+                               const LinearPlan &p, void *workspace, hipStream_t stream) {
+    int32_t *const words = (int32_t *)workspace;
+    const int32_t *order = nullptr;
+    if (p.ordered) {   // [counters][order][tile_start]
+        order = words + kNumCounters;
+        const ScheduleJob job{offsets, nullptr, 64, words + kNumCounters, words + kNumCounters + B};
+        const hipError_t e = launch_schedules(&job, 1, (int)B, words, kNumCounters, stream);
+        if (e != hipSuccess) return e;
+    }
+    float *const carried = (float *)(words + p.order_words);
     switch (D) {
-        case 32: return launch_walks<T, 32>(walks, backward, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
-        case 64: return launch_walks<T, 64>(walks, backward, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
-        case 128: return launch_walks<T, 128>(walks, backward, states, log_decay, offsets, B, H, segments, segment_rows, carried, stream);
+        case 32: return launch_walks<T, 32>(walks, backward, states, log_decay, offsets, order, B, H, p, carried, stream);
+        case 64: return launch_walks<T, 64>(walks, backward, states, log_decay, offsets, order, B, H, p, carried, stream);
+        case 128: return launch_walks<T, 128>(walks, backward, states, log_decay, offsets, order, B, H, p, carried, stream);
         default: return hipErrorInvalidValue;
     }
 }
 
 hipError_t launch_linear_walks(bool f32, const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, int64_t B, int H,
-                               int D, int segments, int segment_rows, float *carried, hipStream_t stream) {
-    return f32 ? launch_walks<float>(walks, backward, states, log_decay, offsets, B, H, D, segments, segment_rows, carried, stream)
-               : launch_walks<__bf16>(walks, backward, states, log_decay, offsets, B, H, D, segments, segment_rows, carried, stream);
+                               int D, const LinearPlan &p, void *workspace, hipStream_t stream) {
+    return f32 ? launch_walks<float>(walks, backward, states, log_decay, offsets, B, H, D, p, workspace, stream)
+               : launch_walks<__bf16>(walks, backward, states, log_decay, offsets, B, H, D, p, workspace, stream);
 }
 
 template <typename T>

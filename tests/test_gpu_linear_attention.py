@@ -132,10 +132,26 @@ def test_long_samples_in_segments(dtype, D, lengths):
     """Few pairs of long samples: several segments at once, joined through their states."""
     from paper_2409_15373_amd import binding
     case = Case(lengths, 1, D, dtype, seed=D, states=True)
-    assert binding.load().jfa_linear_attention_workspace_bytes(case.B, case.max_len, 1, D, 0) > 0
+    assert binding.load().jfa_linear_attention_workspace_bytes(case.B, case.n, case.max_len, 1, D, 0) > 0
     case.check_forward()
     case.check_backward()
     case.S0 = case.dS = None
+    case.check_forward()
+    case.check_backward()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_samples_longest_first(dtype):
+    """More pairs than places, one of them long: walked in another order than the samples'."""
+    from paper_2409_15373_amd import binding
+    lengths = [int(x) for x in np.random.default_rng(3).integers(0, 9, size=70)]
+    lengths[41], lengths[3] = 600, 0
+    case = Case(lengths, 8, 32, dtype, seed=4, states=True)
+    order_only = binding.load().jfa_linear_attention_workspace_bytes(case.B, 70 * 400, case.max_len, 8, 32, 0)
+    assert 0 < order_only < 4096
+    # room behind the rows decides for the order (rows is the tensors' own number of rows)
+    for name in ("q", "k", "v", "dout"):
+        case.t[name] = torch.cat([case.t[name], torch.full((70 * 400, 8, 32), float("nan"), dtype=dtype, device="cuda")])
     case.check_forward()
     case.check_backward()
 

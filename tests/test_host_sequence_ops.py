@@ -22,13 +22,15 @@ def refused(status, expected, word):
 def test_linear_attention(lib, suffix):
     forward, backward, step = (getattr(lib, f"jfa_linear_attention{x}{suffix}") for x in ("", "_backward", "_step"))
 
-    def call(B=2, max_len=8, H=2, D=64, q=16, state=None, offsets=16, workspace=None, n=0):
-        return forward(q, 16, 16, 16, offsets, B, max_len, H, D, 1.0, state, 16, None, workspace, n, None)
+    def call(B=2, rows=16, max_len=8, H=2, D=64, q=16, state=None, offsets=16, workspace=None, n=0):
+        return forward(q, 16, 16, 16, offsets, B, rows, max_len, H, D, 1.0, state, 16, None, workspace, n, None)
 
     refused(call(B=-1), BAD, "negative")
     refused(call(max_len=-1), BAD, "max_len")
     refused(call(max_len=1 << 31), BAD, "max_len")
+    refused(call(rows=-1), BAD, "rows")
     refused(call(H=0), BAD, "H = 0")
+    refused(call(H=1 << 15), UNSUPPORTED, "H * D")
     refused(call(D=48), UNSUPPORTED, "D = 48")
     refused(call(B=(1 << 22) + 1, H=1), UNSUPPORTED, "exceeds")
     refused(call(B=1 << 62, H=8), UNSUPPORTED, "exceeds")
@@ -38,15 +40,15 @@ def test_linear_attention(lib, suffix):
     refused(call(offsets=None), BAD, "null")
     assert call(B=0, q=None, offsets=None) == OK
     # a long sample needs a workspace
-    need = binding.load().jfa_linear_attention_workspace_bytes(1, 100000, 1, 64, 0)
+    need = binding.load().jfa_linear_attention_workspace_bytes(1, 100000, 100000, 1, 64, 0)
     assert need > 0
-    refused(call(B=1, max_len=100000, H=1), BAD, "workspace")
-    refused(call(B=1, max_len=100000, H=1, workspace=16, n=need - 1), BAD, "workspace")
-    refused(call(B=1, max_len=100000, H=1, workspace=8, n=need), BAD, "aligned")
-    refused(backward(16, 16, 16, 16, 16, 16, 2, 8, 2, 64, 1.0, None, None, 16, None, 16, None, None, 0, None), BAD, "null")
-    refused(backward(16, 16, 16, 16, 16, 16, 2, 8, 2, 96, 1.0, None, None, 16, 16, 16, None, None, 0, None), UNSUPPORTED, "D = 96")
-    refused(backward(16, 16, 16, 16, 16, 16, 2, 8, 2, 64, 1.0, None, None, 16, 16, 16, 24, None, 0, None), BAD, "state")
-    refused(backward(16, 16, 16, 16, 16, 16, 1, 100000, 1, 64, 1.0, None, None, 16, 16, 16, None, 16, 16, None), BAD, "workspace")
+    refused(call(B=1, rows=100000, max_len=100000, H=1), BAD, "workspace")
+    refused(call(B=1, rows=100000, max_len=100000, H=1, workspace=16, n=need - 1), BAD, "workspace")
+    refused(call(B=1, rows=100000, max_len=100000, H=1, workspace=8, n=need), BAD, "aligned")
+    refused(backward(16, 16, 16, 16, 16, 16, 2, 16, 8, 2, 64, 1.0, None, None, 16, None, 16, None, None, 0, None), BAD, "null")
+    refused(backward(16, 16, 16, 16, 16, 16, 2, 16, 8, 2, 96, 1.0, None, None, 16, 16, 16, None, None, 0, None), UNSUPPORTED, "D = 96")
+    refused(backward(16, 16, 16, 16, 16, 16, 2, 16, 8, 2, 64, 1.0, None, None, 16, 16, 16, 24, None, 0, None), BAD, "state")
+    refused(backward(16, 16, 16, 16, 16, 16, 1, 100000, 100000, 1, 64, 1.0, None, None, 16, 16, 16, None, 16, 16, None), BAD, "workspace")
     refused(step(16, 16, 16, 16, 2, 2, 64, 1.0, None, 16, 16, None), BAD, "null")
     refused(step(16, 16, 16, 16, 2, 2, 64, 1.0, 16, 16, 24, None), BAD, "aligned")
     refused(step(16, 16, 16, 16, 2, 2, 65, 1.0, 16, 16, 16, None), UNSUPPORTED, "D = 65")
@@ -54,13 +56,18 @@ def test_linear_attention(lib, suffix):
 
 
 def test_the_workspace_of_linear_attention_is_bounded():
-    """It holds states for a few segments per compute unit, whatever the samples' length; many samples need none."""
+    """Samples of like lengths need none; of others, an order of them, or states between segments: as many bytes as a bf16 tensor of that many rows at
+    most, whatever bound on the lengths is given."""
     size = binding.load().jfa_linear_attention_workspace_bytes
-    assert size(4096, 1 << 20, 8, 128, 1) == 0
+    assert size(4096, 4096 << 10, 1 << 10, 8, 128, 1) == 0
+    assert 0 < size(512, 200000, 1024, 4, 128, 0) == size(512, 200000, 1024, 4, 128, 1) < 10000   # an order
     for B, H in [(1, 1), (3, 7), (64, 8)]:
         for D in (32, 64, 128):
-            assert size(B, 1 << 30, H, D, 0) <= (512 + 2 * B * H) * D * D * 4
-    assert size(4, 64, 2, 64, 0) == 0 and size(0, 64, 2, 64, 0) == 0 and size(4, 64, 2, 63, 0) == 0
+            for rows in (2000, 1 << 20):
+                assert size(B, rows, 1 << 30, H, D, 0) <= rows * H * D * 2 * D // 128
+                assert size(B, rows, 1 << 30, H, D, 1) <= rows * H * D * 4 * D // 128
+            assert size(1, 1, 1 << 30, H, D, 0) == 0 < size(1, 1 << 20, 1 << 30, 1, D, 0)
+    assert size(4, 256, 64, 2, 64, 0) == 0 and size(0, 0, 64, 2, 64, 0) == 0 and size(4, 256, 64, 2, 63, 0) == 0
 
 
 @pytest.mark.parametrize("suffix", ["", "_f32"])
