@@ -838,6 +838,7 @@ struct LinearPlan {
     int64_t segment_rows;
     int between;             // states between segments, for each walk and head
     bool ordered;            // longest samples first
+    bool apart;              // the backward's three walks in workgroups of their own
     int64_t order_words, bytes;   // of the workspace: the order, all of it
 };
 LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, bool backward);

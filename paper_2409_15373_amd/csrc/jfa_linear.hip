@@ -127,19 +127,25 @@ __device__ inline int64_t state_between(int walk, int h, int H, int between, int
 }  // namespace
 
 // A workgroup takes one (sample, head, segment), blockIdx.x, through ROLES walks that go the same way over the same tensors: one of them (walk
-// blockIdx.y), or the two that give dk and dv, which share the tiles of q and dout.  Each walk has D / 32 waves; wave w of it owns columns
-// 32 w .. 32 w + 31 of the state and of the outputs.
+// blockIdx.y), or the two that give dk and dv, which share the tiles of q and dout.  Each walk has D / 32 waves, each of which owns 32 columns of
+// the state and of the outputs.
+// fp32, D = 64 and 128, one walk: twice as many, two to a strip of 32 columns with half of the state's rows each (linear_parts): the fp32 matrix instructions are what
+// a chunk waits for (64 clocks for 4096 products), and this way a wave has 48 of them instead of 112 in a chunk (D = 64; D = 128: 80 of 208).  P is summed over its
+// contraction, a step of 16 for each wave, and out over the two halves, through LDS.  (A sample of 256 rows, D = 64, 34 -> 25 us.  Two walks: there 8 waves a compute
+// unit have both forms' room, and 2048 of 256 rows took 443 us for all gradients, 409 without.)
 // bf16: what is rounded in front of a product (P, the state as a factor of out, the decayed rows of C) is split into two bf16 numbers, 16 bits in
 // all, so that a result's error is its own rounding (one bf16 number each: 1.65 times that, root mean square); kParts = 3, exact, for the decayed
 // rows where the state is itself a result.  The matrix instructions have the time: they are busy a third of a chunk's way through memory.
 // kStateOnly: the state that a segment adds to, for those with a segment after them, into `carried`.
+template <typename T, int D, int ROLES> __host__ __device__ constexpr int linear_parts() { return sizeof(T) == 4 && D > 32 && ROLES == 1 ? 2 : 1; }
 template <typename T, int D, int ROLES, int kParts, bool kStateOnly>
-__global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
+__global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES == 1 ? 2 : 1), 2) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
                                                                        const int32_t *__restrict__ order, int B, int H, int segments, int segment_rows, int between,
                                                                        float *__restrict__ carried) {
     typedef Elem<T> E;
     typedef typename E::Operand Operand;
-    constexpr int kRows = E::kRows, kSize = (int)sizeof(T), kStateTiles = D / 32, kSteps = D / 16, kSplit = E::kSplit, kWaves = kStateTiles * ROLES;
+    constexpr int kRows = E::kRows, kSize = (int)sizeof(T), kStateTiles = D / 32, kSteps = D / 16, kSplit = E::kSplit;
+    constexpr int KS = linear_parts<T, D, ROLES>(), kWalkWaves = kStateTiles * KS, kWaves = kWalkWaves * ROLES, kMine = kStateTiles / KS;   // kMine: state tiles of a wave
     constexpr int kTiles = kRows / 32, kPTiles = kTiles * (kTiles + 1) / 2;
     constexpr int kChunks = D * kSize / 16, kTileBytes = kRows * kChunks * 16, kLoads = kRows * kChunks / (64 * kWaves);   // 16-byte chunks of a row; copies of a tile per wave
     // Places of tiles.  A is free for the next chunk's once the state's product with it is done, in the middle of a chunk.  B and, of two walks, C (their B
@@ -150,11 +156,13 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
     // one tile) has it in registers.
     constexpr bool kShareP = !kStateOnly && kPTiles > 1 && kStateTiles > 1;
     constexpr int kPBytes = kShareP ? kPTiles * 2 * kSplit * 1024 : 0;
-    __shared__ __attribute__((aligned(16))) char lds[kPlaces * kTileBytes + ROLES * kPBytes];
+    static_assert(KS == 1 || (kTiles == 1 && kSteps == kWalkWaves), "a step of P's contraction for each wave");
+    constexpr int kXBytes = KS > 1 && !kStateOnly ? kWalkWaves * (4 + 2) * 1024 : 0;   // a wave's part of P, half of its part of out
+    __shared__ __attribute__((aligned(16))) char lds[kPlaces * kTileBytes + ROLES * (kPBytes + kXBytes)];
     __shared__ float powers[ROLES][2][2 * kRows];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int role = ROLES == 2 ? wave / kStateTiles : 0, strip = ROLES == 2 ? wave % kStateTiles : wave;
+    const int role = wave / kWalkWaves, walk_wave = wave % kWalkWaves, strip = walk_wave % kStateTiles, part = walk_wave / kStateTiles;
     const int col = lane & 31, half = lane >> 5;
     const int which = ROLES == 2 ? 1 : (int)blockIdx.y;   // the first role's walk
     const LinearWalk &walk = walks.walk[which + role];
@@ -169,7 +177,7 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
     const int64_t t0 = (int64_t)segment * segment_rows;   // rows are counted in the order of the walk
     const bool last = t0 + segment_rows >= L;
     if (kStateOnly ? last || segment == segments - 1 : (t0 >= L && segment > 0)) return;
-    if (segments > 1 && first / segment_rows + segment > between) return;   // (more rows than the caller said there were)
+    if (segments > 1 && first / segment_rows + segment + (kStateOnly ? 1 : 0) > between) return;   // (more rows than the caller said there were)
     const int64_t left = L - t0;
     const int n = (int)(left < segment_rows ? left : segment_rows);   // rows of this segment; 0 for an empty sample
     const bool reverse = walk.reverse;
@@ -177,9 +185,9 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
     float *const passed = carried + state_between(walk.carried, h, H, between, first, segment_rows) * D * D;
     float *const state_out = kStateOnly ? passed + (int64_t)segment * D * D : last && walk.state_out ? walk.state_out + (int64_t)pair * D * D : nullptr;
 
-    f32x16 S[kStateTiles];   // tile m: rows 32 m .. (dimension of B), columns 32 strip .. (dimension of C)
+    f32x16 S[kMine];   // tile m: rows 32 (kMine part + m) .. (dimension of B), columns 32 strip .. (dimension of C)
 #pragma unroll
-    for (int m = 0; m < kStateTiles; ++m)
+    for (int m = 0; m < kMine; ++m)
 #pragma unroll
         for (int v = 0; v < 16; ++v) S[m][v] = 0.0f;
     if (!kStateOnly) {
@@ -187,10 +195,10 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
         if (from) {
             const bool transposed = segment == 0 ? walk.transposed : walk.carried_transposed;
 #pragma unroll
-            for (int m = 0; m < kStateTiles; ++m)
+            for (int m = 0; m < kMine; ++m)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const int r = m * 32 + exchanged(acc_row(v, half)), c = strip * 32 + col;
+                    const int r = (part * kMine + m) * 32 + exchanged(acc_row(v, half)), c = strip * 32 + col;
                     S[m][v] = from[transposed ? c * D + r : r * D + c];
                 }
         }
@@ -222,12 +230,13 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
             for (int u = 0; u < kLoads; ++u) bd_dma16(base, offset_of(u, rows), dst + u * kWaves * 1024);
         }
     };
-    const int row_base = E::template rows_base<D>(lane), col_base = E::template cols_base<D, false>(lane) ^ (strip * 32 * kSize), col_base_b = E::template cols_base<D, true>(lane);
+    const int row_base = E::template rows_base<D>(lane), col_base = E::template cols_base<D, false>(lane) ^ (strip * 32 * kSize), 
+              col_base_b = E::template cols_base<D, true>(lane) ^ (part * kMine * 32 * kSize);
 
     // powers[0][kRows + x]: in_scale g^x, zero for negative x: P's factors.  powers[1]: with the decay after a chunk's last row, `tail`: the state's.
     const int tail = reverse ? 1 : 0;
     float (*const my_powers)[2 * kRows] = powers[role];
-    for (int i = strip * 64 + lane; i < 2 * 2 * kRows; i += 64 * kStateTiles) {
+    for (int i = walk_wave * 64 + lane; i < 2 * 2 * kRows; i += 64 * kWalkWaves) {
         const int x = i % (2 * kRows) - kRows;
         my_powers[i / (2 * kRows)][x + kRows] = x < 0 ? 0.0f : walk.in_scale * power(lg, x + (i < 2 * kRows ? 0 : tail));
     }
@@ -272,6 +281,7 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
         const char *const at = lds + role * kTileBytes;
         const char *const bt = lds + (ROLES == 2 ? 2 + 2 * role + turn : 2 + turn) * kTileBytes, *const ct = lds + (ROLES == 2 ? 4 - 2 * role + turn : 1) * kTileBytes;
         char *const pt = lds + kPlaces * kTileBytes + role * kPBytes;
+        char *const px = lds + kPlaces * kTileBytes + role * kXBytes, *const ox = px + kWalkWaves * 4096;   // KS > 1
         Operand c[2 * kTiles];   // the chunk's rows of C, this wave's columns
         if (kStateOnly) {
             c_is_there();
@@ -280,7 +290,7 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
         }
         if (!kStateOnly) {
             // P^T, tiles (rows j of B) x (columns i of A), zero above the diagonal
-            Operand P[kShareP ? 1 : kPTiles][2][kSplit];
+            Operand P[kShareP || KS > 1 ? 1 : kPTiles][2][kSplit];
             const float *const near = my_powers[0] + kRows + col - 4 * half;   // [-(8 g + e)]: g^(i - j)
             auto weighted = [&](f32x16 &p, int t, auto &&put) {   // t: 0, 2 on the diagonal, 1 below it; put(contraction step, part, operand)
 #pragma unroll
@@ -299,7 +309,15 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
                     }
                 }
             };
-            if constexpr (kShareP) {
+            if constexpr (KS > 1) {
+                f32x16 p;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) p[v] = 0.0f;
+                const int base = row_base ^ (walk_wave * 16 * kSize);
+                p = E::product(E::template rows<D>(bt, base, 0, 0), E::template rows<D>(at, base, 0, 0), p);
+#pragma unroll
+                for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4 *>(px + (walk_wave * 4 + g) * 1024 + lane * 16) = f32x4{p[4 * g], p[4 * g + 1], p[4 * g + 2], p[4 * g + 3]};
+            } else if constexpr (kShareP) {
 #pragma unroll
                 for (int t = 0; t < kPTiles; ++t) {
                     if (t % kStateTiles != strip) continue;
@@ -356,15 +374,16 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
             for (int ti = 0; ti < kTiles; ++ti)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[ti][v] = 0.0f;
+            const int state_base = row_base ^ (part * (kSteps / KS) * 16 * kSize);   // from this wave's first row of the state on
             Operand a[2][kTiles];
             auto read = [&](int ks) {
 #pragma unroll
-                for (int ti = 0; ti < kTiles; ++ti) a[ks & 1][ti] = E::template rows<D>(at, row_base, ti * 32, ks * 16);
+                for (int ti = 0; ti < kTiles; ++ti) a[ks & 1][ti] = E::template rows<D>(at, state_base, ti * 32, ks * 16);
             };
             read(0);
 #pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) {
-                if (ks + 1 < kSteps) read(ks + 1);
+            for (int ks = 0; ks < kSteps / KS; ++ks) {
+                if (ks + 1 < kSteps / KS) read(ks + 1);
                 __builtin_amdgcn_sched_barrier(0);
                 f32x8 x = eight(S[ks >> 1], (ks & 1) * 8);
 #pragma unroll
@@ -386,6 +405,43 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
             for (int ti = 0; ti < kTiles; ++ti)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[ti][v] *= since[ti];
+            if constexpr (KS > 1) {
+                // this wave's half of P's rows, summed over the waves, with the same rows of C; then its half of out's columns, summed over the two
+                f32x8 x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWalkWaves; ++w) {
+                    const f32x4 lo = *reinterpret_cast<const f32x4 *>(px + (w * 4 + 2 * part) * 1024 + lane * 16), hi = *reinterpret_cast<const f32x4 *>(px + (w * 4 + 2 * part + 1) * 1024 + lane * 16);
+                    x += __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int row = part * 16 + (e >> 2) * 8 + (e & 3);
+                    x[e] = col < row + 4 * half ? 0.0f : x[e] * near[-row];
+                }
+                o[0] = E::product(E::template cols<D>(ct + part * 16 * D * kSize, col_base, 0, 0), E::pack(x), o[0]);
+                f32x8 mine = eight(o[0], 0), others = eight(o[0], 8);
+                if (part) {
+                    const f32x8 swapped = mine;
+                    mine = others;
+                    others = swapped;
+                }
+                *reinterpret_cast<f32x4 *>(ox + (walk_wave * 2) * 1024 + lane * 16) = f32x4{others[0], others[1], others[2], others[3]};
+                *reinterpret_cast<f32x4 *>(ox + (walk_wave * 2 + 1) * 1024 + lane * 16) = f32x4{others[4], others[5], others[6], others[7]};
+                __syncthreads();
+                const int partner = strip + (1 - part) * kStateTiles;
+                if (col < rows) {
+                    char *const dst = reinterpret_cast<char *>((T *)walk.out + low) +
+                                      ((uint32_t)(reverse ? kRows - 1 - col : col) * row_bytes + (uint32_t)(strip * 32 + part * 16 + half * 4) * kSize);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const f32x4 y = *reinterpret_cast<const f32x4 *>(ox + (partner * 2 + g) * 1024 + lane * 16);
+                        E::store4(reinterpret_cast<T *>(dst + g * 8 * kSize), f32x4{(mine[4 * g] + y[0]) * out_scale, (mine[4 * g + 1] + y[1]) * out_scale,
+                                                                                   (mine[4 * g + 2] + y[2]) * out_scale, (mine[4 * g + 3] + y[3]) * out_scale});
+                    }
+                }
+            } else {
 #pragma unroll
             for (int ks = 0; ks < 2 * kTiles; ++ks)
 #pragma unroll
@@ -409,22 +465,23 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
                                   f32x4{o[ti][4 * g] * out_scale, o[ti][4 * g + 1] * out_scale, o[ti][4 * g + 2] * out_scale, o[ti][4 * g + 3] * out_scale});
                 }
             }
+            }
         }
         // S <- g^rows S + (g^(rows - 1 - i) B)^T C, unless nobody looks at it any more
         if (r0 + kRows < n || state_out) {
             const float decay = power(lg, rows);
 #pragma unroll
-            for (int m = 0; m < kStateTiles; ++m)
+            for (int m = 0; m < kMine; ++m)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) S[m][v] *= decay;
             const float *const left = my_powers[1] + rows - 1 - 4 * half;   // of the chunk's row i: [kRows - i]; rows that are not there have zero
-            Operand x[2][kStateTiles];
+            Operand x[2][kMine];
             float weight[2][8];
             auto read = [&](int ks) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) weight[ks & 1][e] = left[kRows - (ks * 16 + (e >> 2) * 8 + (e & 3))];
 #pragma unroll
-                for (int m = 0; m < kStateTiles; ++m) x[ks & 1][m] = E::template cols<D>(bt, col_base_b, m * 32, ks * 16);
+                for (int m = 0; m < kMine; ++m) x[ks & 1][m] = E::template cols<D>(bt, col_base_b, m * 32, ks * 16);
             };
             read(0);
 #pragma unroll
@@ -438,7 +495,7 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
                 for (int part = 0; part < kParts; ++part) {
                     const Operand z = E::pack(y);
 #pragma unroll
-                    for (int m = 0; m < kStateTiles; ++m) S[m] = E::product(x[ks & 1][m], z, S[m]);
+                    for (int m = 0; m < kMine; ++m) S[m] = E::product(x[ks & 1][m], z, S[m]);
                     if (part + 1 < kParts) y -= E::widen(z);
                 }
             }
@@ -447,10 +504,10 @@ __global__ __launch_bounds__(2 * D * ROLES, 2) void linear_walk_kernel(LinearWal
     if (state_out) {
         const bool transposed = !kStateOnly && walk.transposed;
 #pragma unroll
-        for (int m = 0; m < kStateTiles; ++m)
+        for (int m = 0; m < kMine; ++m)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int r = m * 32 + exchanged(acc_row(v, half)), c = strip * 32 + col;
+                const int r = (part * kMine + m) * 32 + exchanged(acc_row(v, half)), c = strip * 32 + col;
                 state_out[transposed ? c * D + r : r * D + c] = S[m][v];
             }
     }
@@ -532,6 +589,8 @@ __global__ __launch_bounds__(256) void linear_step_kernel(const T *__restrict__ 
 // the two passes over a segment.  8 x 2 samples of up to 16000 rows (D = 128) otherwise: 250 chunks one after the other.
 // Many samples of different lengths that are not cut are walked longest first: the walks that are left at the end are short ones (512 x 4 samples of up to 1024
 // rows, forward 307 -> 260 us); the order is made by the attention's scheduler.
+// The backward's three walks are three workgroups where all of their rows take no longer than the longest sample's walk; else dk and dv are one, which reads 6 tensors
+// instead of 8 (64 samples of 600 rows, D = 64, fp32 161 -> 58 us, bf16 62 -> 32).  fp32 at D = 128: three, two have no room on a compute unit.
 LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, bool backward) {
     constexpr int64_t kPlaces = 2 * 256, kLeastSegment = 256, kMostSegment = 1024;
     LinearPlan p;
@@ -549,6 +608,7 @@ LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, b
             p.between = (int)(rows / segment);
         }
     }
+    p.apart = 3 * W < max_len;
     p.ordered = p.segments == 1 && B > 1 && B * H > kPlaces && max_len >= 512 && (double)max_len * B > 1.2 * rows;
     p.order_words = p.ordered ? (2 * B + 1 + kNumCounters + 63) / 64 * 64 : 0;
     p.bytes = p.order_words * 4 + (int64_t)(backward ? 2 : 1) * H * p.between * D * D * 4;
@@ -557,26 +617,31 @@ LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, b
 
 template <typename T, int D, int kParts>
 static void launch_walks(const LinearWalks &walks, bool backward, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H, int segments,
-                         int segment_rows, int between, float *carried, hipStream_t stream) {
+                         int segment_rows, int between, bool apart, float *carried, hipStream_t stream) {
     const unsigned blocks = (unsigned)((D * sizeof(T) < 128 ? (B * segments + 7) / 8 * 8 : B * segments) * H);
+    constexpr int kThreads = 2 * D * linear_parts<T, D, 1>();
     if (segments > 1) {   // walk 0, and of the two that go back, which have one state, walk 2
         const LinearWalks states{{walks.walk[0], walks.walk[2], walks.walk[2]}};
         const int n = backward ? 2 : 1;
-        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, true>), dim3(blocks, n), dim3(2 * D), 0, stream, states, log_decay, offsets, order, (int)B, H, segments, segment_rows, between, carried);
+        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, true>), dim3(blocks, n), dim3(kThreads), 0, stream, states, log_decay, offsets, order, (int)B, H, segments, segment_rows,
+                           between, carried);
         hipLaunchKernelGGL(linear_carry_kernel, dim3((unsigned)(B * H * (D * D / 1024)), n), dim3(256), 0, stream, states, log_decay, offsets, H, D, segments, segment_rows,
                            between, carried);
     }
-    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, false>), dim3(blocks), dim3(2 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows, between, carried);
-    if (backward)
-        hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows, between, carried);
+    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, false>), dim3(blocks, backward && apart ? 3 : 1), dim3(kThreads), 0, stream, walks, log_decay, offsets, order, (int)B, H,
+                       segments, segment_rows, between, carried);
+    if constexpr (sizeof(T) == 2 || D < 128)
+        if (backward && !apart)
+            hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows,
+                               between, carried);
 }
 template <typename T, int D>
 static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H,
                                const LinearPlan &p, float *carried, hipStream_t stream) {
     const int segment_rows = (int)p.segment_rows;
-    if constexpr (sizeof(T) == 4) launch_walks<T, D, 1>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, carried, stream);
-    else if (states) launch_walks<T, D, 3>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, carried, stream);
-    else launch_walks<T, D, 2>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, carried, stream);
+    if constexpr (sizeof(T) == 4) launch_walks<T, D, 1>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, p.apart || (sizeof(T) == 4 && D == 128), carried, stream);
+    else if (states) launch_walks<T, D, 3>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, p.apart || (sizeof(T) == 4 && D == 128), carried, stream);
+    else launch_walks<T, D, 2>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, p.apart || (sizeof(T) == 4 && D == 128), carried, stream);
     return hipGetLastError();
 }
 
