@@ -33,14 +33,14 @@ template <typename T, int VEC> __device__ inline void em_load(const T *p, float 
         for (int e = 0; e < VEC; ++e) x[e] = (float)v[e];
     }
 }
-template <typename T, int VEC> __device__ inline void em_store(T *p, const float (&x)[VEC]) {
+template <typename T, int VEC, bool PAST = false> __device__ inline void em_store(T *p, const float (&x)[VEC]) {
     typename EmVec<T, VEC>::Type v;
     if constexpr (VEC == 1) v = (T)x[0];
     else {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) v[e] = (T)x[e];
     }
-    *reinterpret_cast<typename EmVec<T, VEC>::Type *>(p) = v;
+    store_streaming<PAST>(reinterpret_cast<typename EmVec<T, VEC>::Type *>(p), v);
 }
 
 __device__ inline int64_t em_rows_there(const int64_t *offsets, int64_t B, int64_t rows) {
@@ -49,11 +49,14 @@ __device__ inline int64_t em_rows_there(const int64_t *offsets, int64_t B, int64
     return have < 0 ? 0 : have < rows ? have : rows;
 }
 
-// LANES lanes per row, kInFlight rows at a time.
-template <typename T, typename Id, int VEC, int LANES>
+// LANES lanes per row, kInFlight rows at a time (2, 4 and 8: 29.7, 32.1 and 36.4 us for 322248 rows of 128).  PAST: rows are stored past the L2, for
+// what has more of them than the L2s hold: the table's frequent rows stay (131072 rows of 512, 37 -> 25 us).
+constexpr int kInFlight = 2;
+constexpr int64_t kL2Bytes = 32 << 20;
+template <typename T, typename Id, int VEC, int LANES, bool PAST>
 __global__ __launch_bounds__(kEmThreads) void embedding_kernel(const T *__restrict__ table, const Id *__restrict__ ids, const int64_t *__restrict__ offsets,
                                                                int64_t B, int64_t rows, int64_t V, int64_t N, float scale, T *__restrict__ out) {
-    constexpr int kPerBlock = kEmThreads / LANES, kInFlight = 4;
+    constexpr int kPerBlock = kEmThreads / LANES;
     const int64_t n = em_rows_there(offsets, B, rows);
     const int lane = threadIdx.x % LANES;
     for (int64_t i0 = (int64_t)blockIdx.x * kPerBlock * kInFlight + threadIdx.x / LANES; i0 < n; i0 += (int64_t)gridDim.x * kPerBlock * kInFlight) {
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(kEmThreads) void embedding_kernel(const T *__restri
             }
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u)
-                if (i0 + u * kPerBlock < n) em_store<T, VEC>(out + (i0 + u * kPerBlock) * N + c, x[u]);
+                if (i0 + u * kPerBlock < n) em_store<T, VEC, PAST>(out + (i0 + u * kPerBlock) * N + c, x[u]);
         }
     }
 }
@@ -100,19 +103,20 @@ struct Clearing {
     char *dst;
     int64_t bytes, from, to;
 };
+// Past the L2, where the rows of dout, which the block sums read next, may be (1000003 x 128: block sums 38 -> 21 us, and the next pass' lookup 30 -> 18).
 constexpr int kClearBytes = kSortThreads * 16 * 4;
 __device__ inline void clear_share(const Clearing &c, int64_t unit) {
     if (unit >= c.to) return;
     const int64_t at = unit * kClearBytes;
     if (((uintptr_t)c.dst & 15) == 0 && at + kClearBytes <= c.bytes) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) *reinterpret_cast<u32x4 *>(c.dst + at + (u * kSortThreads + threadIdx.x) * 16) = u32x4{0, 0, 0, 0};
+        for (int u = 0; u < 4; ++u) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4 *>(c.dst + at + (u * kSortThreads + threadIdx.x) * 16));
         return;
     }
     for (int64_t i = at + threadIdx.x * 2; i < at + kClearBytes && i < c.bytes; i += kSortThreads * 2) *reinterpret_cast<uint16_t *>(c.dst + i) = 0;
 }
 
-// counts[bin * tiles + tile].
+// counts[tile][bin].
 template <bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortSource s, int shift, int bits, int tiles, uint32_t *__restrict__ counts, Clearing clearing) {
     __shared__ uint32_t bins[1 << kEmMostBits];
@@ -124,32 +128,42 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortSource s, 
     const int first = (int)blockIdx.x * kEmTile, end = s.rows - first < kEmTile ? s.rows : first + kEmTile;
     for (int i = first + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&bins[(sort_key<FIRST>(s, there, i) >> shift) & (n_bins - 1)], 1u);
     __syncthreads();
-    for (int i = threadIdx.x; i < n_bins; i += kSortThreads) counts[(int64_t)i * tiles + blockIdx.x] = bins[i];
+    for (int i = threadIdx.x; i < n_bins; i += kSortThreads) counts[(int64_t)blockIdx.x * n_bins + i] = bins[i];
 }
 
-// A wave per bin: counts -> the counts of the tiles before, and the bin's total.
+// counts -> the counts of the tiles before, and the bins' totals: 64 bins per workgroup, a sixteenth of the tiles for each of its waves.
 __global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(int n_bins, int tiles, uint32_t *__restrict__ counts, uint32_t *__restrict__ totals, Clearing clearing) {
-    const int own = (n_bins + kSortThreads / 64 - 1) / (kSortThreads / 64);
+    constexpr int kWaves = kSortThreads / 64;
+    __shared__ uint32_t sums[kWaves][64];
+    const int own = (n_bins + 63) / 64;
     if ((int)blockIdx.x >= own) return clear_share(clearing, clearing.from + blockIdx.x - own);
-    const int bin = blockIdx.x * (kSortThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (bin >= n_bins) return;
-    uint32_t *row = counts + (int64_t)bin * tiles, carry = 0;
-    for (int t0 = 0; t0 < tiles; t0 += 64) {
-        const uint32_t mine = t0 + lane < tiles ? row[t0 + lane] : 0;
-        uint32_t sum = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t y = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += y;
-        }
-        if (t0 + lane < tiles) row[t0 + lane] = carry + sum - mine;
-        carry += __shfl(sum, 63, 64);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bin = blockIdx.x * 64 + lane;
+    const int each = (tiles + kWaves - 1) / kWaves, first = wave * each, end = first + each < tiles ? first + each : tiles;
+    uint32_t sum = 0;
+    if (bin < n_bins) {
+#pragma unroll 8
+        for (int t = first; t < end; ++t) sum += counts[(int64_t)t * n_bins + bin];
     }
-    if (lane == 0) totals[bin] = carry;
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (bin >= n_bins) return;
+    uint32_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) before += sums[w][lane];
+        total += sums[w][lane];
+    }
+    for (int t = first; t < end; ++t) {
+        const uint32_t c = counts[(int64_t)t * n_bins + bin];
+        counts[(int64_t)t * n_bins + bin] = before;
+        before += c;
+    }
+    if (wave == 0) totals[bin] = total;
 }
 
 // Every key and position to its place.  A wave has a sixteenth of the tile in order; equal digits of a wave's 64 keys are ranked by ballots.
-// counts and totals may be null where there is one tile.
+// totals: null where nobody has scanned the counts.  Up to kFewTiles tiles a workgroup adds its bins' counts itself, in less time than a launch takes.
+constexpr int kFewTiles = 128;
 template <bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, int shift, int bits, int tiles, const uint32_t *__restrict__ counts,
                                                                   const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys, uint32_t *__restrict__ positions,
@@ -174,11 +188,22 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, 
     // a thread per bin: what the waves have of it, then where the bin starts: behind the bins before it
     static_assert(1 << kEmMostBits <= kSortThreads, "a thread per bin");
     const int bin = threadIdx.x;
-    uint32_t here = 0, total = 0;
+    uint32_t here = 0, before = 0, total = 0;
     if (bin < n_bins) {
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) here += next[w][bin];
-        total = totals ? totals[bin] : here;
+        if (totals) {
+            before = counts[(int64_t)blockIdx.x * n_bins + bin];
+            total = totals[bin];
+        } else if (tiles == 1) total = here;
+        else {
+#pragma unroll 16
+            for (int t = 0; t < tiles; ++t) {
+                const uint32_t c = counts[(int64_t)t * n_bins + bin];
+                total += c;
+                before += t < (int)blockIdx.x ? c : 0;
+            }
+        }
     }
     uint32_t sum = total;
 #pragma unroll
@@ -191,7 +216,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, 
     uint32_t at_bin = sum - total;
     for (int w = 0; w < wave; ++w) at_bin += wave_totals[w];
     if (bin < n_bins) {
-        if (counts) at_bin += counts[(int64_t)bin * tiles + blockIdx.x];
+        at_bin += before;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const uint32_t c = next[w][bin];
@@ -448,10 +473,13 @@ template <typename T, typename Launch> hipError_t em_spread(int64_t N, bool alig
 template <typename T, typename Id>
 hipError_t embedding_t(const T *table, const Id *ids, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale, T *out, hipStream_t stream) {
     return em_spread<T>(N, aligned16(table, out), [&](auto vec, auto lanes) {
-        constexpr int VEC = decltype(vec)::value, L = decltype(lanes)::value, kRows = kEmThreads / L * 4;
+        constexpr int VEC = decltype(vec)::value, L = decltype(lanes)::value, kRows = kEmThreads / L * kInFlight;
         const int64_t need = (rows + kRows - 1) / kRows;
-        hipLaunchKernelGGL((embedding_kernel<T, Id, VEC, L>), dim3((unsigned)(need < 8192 ? need : 8192)), dim3(kEmThreads), 0, stream, table, ids, offsets, B, rows, V, N, scale,
-                           out);
+        const dim3 grid((unsigned)(need < 16384 ? need : 16384)), threads(kEmThreads);
+        if (rows * N * (int64_t)sizeof(T) > kL2Bytes)
+            hipLaunchKernelGGL((embedding_kernel<T, Id, VEC, L, true>), grid, threads, 0, stream, table, ids, offsets, B, rows, V, N, scale, out);
+        else
+            hipLaunchKernelGGL((embedding_kernel<T, Id, VEC, L, false>), grid, threads, 0, stream, table, ids, offsets, B, rows, V, N, scale, out);
         return hipGetLastError();
     });
 }
@@ -488,11 +516,12 @@ hipError_t embedding_backward_t(const T *dout, const void *ids, bool ids64, cons
                                 T *dtable, uint32_t *ws, hipStream_t stream) {
     const EmPlan p = em_plan(rows, V, N);
     const dim3 threads(kSortThreads);
-    uint32_t *const counts = p.tiles > 1 ? ws + p.counts : nullptr, *const totals = p.tiles > 1 ? ws + p.totals : nullptr;
+    const bool scan = p.tiles > kFewTiles;
+    uint32_t *const counts = ws + p.counts, *const totals = scan ? ws + p.totals : nullptr;
     SortSource s{ids, nullptr, nullptr, offsets, B, V, (int)rows, ids64};
     // every launch of the sort clears a share of the table
     const int64_t table_bytes = V * N * (int64_t)sizeof(T), units = (table_bytes + kClearBytes - 1) / kClearBytes;
-    const int launches = p.passes * (p.tiles > 1 ? 3 : 1);
+    const int launches = p.passes * (scan ? 3 : p.tiles > 1 ? 2 : 1);
     int launch = 0;
     const auto share = [&]() {
         const Clearing c{(char *)dtable, table_bytes, units * launch / launches, units * (launch + 1) / launches};
@@ -512,8 +541,10 @@ hipError_t embedding_backward_t(const T *dout, const void *ids, bool ids64, cons
             const Clearing c = share();
             if (pass == 0) hipLaunchKernelGGL((sort_count_kernel<true>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, c);
             else hipLaunchKernelGGL((sort_count_kernel<false>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, c);
-            const Clearing d = share();
-            hipLaunchKernelGGL(sort_scan_kernel, grid((bins + kSortThreads / 64 - 1) / (kSortThreads / 64), d), threads, 0, stream, bins, p.tiles, counts, totals, d);
+        }
+        if (scan) {
+            const Clearing c = share();
+            hipLaunchKernelGGL(sort_scan_kernel, grid((bins + 63) / 64, c), threads, 0, stream, bins, p.tiles, counts, totals, c);
         }
         const Clearing c = share();
         if (pass == 0) hipLaunchKernelGGL((sort_place_kernel<true>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions, c);
