@@ -834,7 +834,6 @@ int linear_launch(const char *who, bool f32, const jfa::LinearWalks &walks, bool
     if (workspace_bytes < need || (need && !workspace))
         return fail(JFA_ERR_INVALID_ARG, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? workspace_bytes : 0, need);
     if (need && misaligned(workspace)) return fail(JFA_ERR_INVALID_ARG, "%s: the workspace is not 16-byte aligned", who);
-    if (B * H * plan.segments >= (int64_t)1 << 24) return fail(JFA_ERR_UNSUPPORTED, "%s: B = %lld samples of up to %lld rows are too many", who, (long long)B, (long long)max_len);
     ScopedTimer tm(backward ? "linear_attention_bwd" : "linear_attention", s);
     const hipError_t e = jfa::launch_linear_walks(f32, walks, backward, states, log_decay, offsets, B, H, D, plan, workspace, s);
     return e == hipSuccess ? JFA_OK : hip_fail("linear attention kernel", e);
@@ -870,6 +869,7 @@ int linear_step(const char *who, bool f32, const void *q, const void *k, const v
     if (st != JFA_OK || B == 0) return st;
     const void *tensors[] = {q, k, v, out, state, new_state, log_decay};
     if ((st = linear_pointers(who, tensors, 7, nullptr, 0)) != JFA_OK) return st;
+    if (B * H * (D / 32) >= (int64_t)1 << 24) return fail(JFA_ERR_UNSUPPORTED, "%s: B * H = %lld is too large for D = %d", who, (long long)B * H, D);
     ScopedTimer tm("linear_attention_step", s);
     const hipError_t e = jfa::launch_linear_step(f32, q, k, v, log_decay, B, H, D, scale, state, out, new_state, s);
     return e == hipSuccess ? JFA_OK : hip_fail("linear attention step kernel", e);

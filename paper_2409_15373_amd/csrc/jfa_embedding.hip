@@ -8,8 +8,8 @@
 // left as a partial sum, and those are added by the lanes of the block that the id begins in, kEmSuper of them at once where one
 // id has that many.  The table's other rows are zeros: the sort, a few dozen workgroups that wait for memory, has the chip to itself, so its launches
 // carry workgroups that clear the whole table (a row that is written again costs less than finding out that it will be).
-#include "jfa_common.h"
 #include "jfa_mfma.h"
+#include "jfa_rows.h"
 
 namespace jfa {
 
@@ -22,33 +22,6 @@ constexpr int kEmSuper = 64;     // blocks that are added at once
 constexpr int kEmMostBits = 10;  // of a sort's digit
 constexpr int kSortThreads = 1024;
 
-template <typename T, int VEC> struct EmVec { typedef T Type __attribute__((ext_vector_type(VEC))); };
-template <typename T> struct EmVec<T, 1> { typedef T Type; };
-
-template <typename T, int VEC> __device__ inline void em_load(const T *p, float (&x)[VEC]) {
-    const typename EmVec<T, VEC>::Type v = *reinterpret_cast<const typename EmVec<T, VEC>::Type *>(p);
-    if constexpr (VEC == 1) x[0] = (float)v;
-    else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[e] = (float)v[e];
-    }
-}
-template <typename T, int VEC, bool PAST = false> __device__ inline void em_store(T *p, const float (&x)[VEC]) {
-    typename EmVec<T, VEC>::Type v;
-    if constexpr (VEC == 1) v = (T)x[0];
-    else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = (T)x[e];
-    }
-    store_streaming<PAST>(reinterpret_cast<typename EmVec<T, VEC>::Type *>(p), v);
-}
-
-__device__ inline int64_t em_rows_there(const int64_t *offsets, int64_t B, int64_t rows) {
-    if (!offsets) return rows;
-    const int64_t have = offsets[B];
-    return have < 0 ? 0 : have < rows ? have : rows;
-}
-
 // LANES lanes per row, kInFlight rows at a time (2, 4 and 8: 29.7, 32.1 and 36.4 us for 322248 rows of 128).  PAST: rows are stored past the L2, for
 // what has more of them than the L2s hold: the table's frequent rows stay (131072 rows of 512, 37 -> 25 us).
 constexpr int kInFlight = 2;
@@ -57,7 +30,7 @@ template <typename T, typename Id, int VEC, int LANES, bool PAST>
 __global__ __launch_bounds__(kEmThreads) void embedding_kernel(const T *__restrict__ table, const Id *__restrict__ ids, const int64_t *__restrict__ offsets,
                                                                int64_t B, int64_t rows, int64_t V, int64_t N, float scale, T *__restrict__ out) {
     constexpr int kPerBlock = kEmThreads / LANES;
-    const int64_t n = em_rows_there(offsets, B, rows);
+    const int64_t n = rows_there(offsets, B, rows);
     const int lane = threadIdx.x % LANES;
     for (int64_t i0 = (int64_t)blockIdx.x * kPerBlock * kInFlight + threadIdx.x / LANES; i0 < n; i0 += (int64_t)gridDim.x * kPerBlock * kInFlight) {
         int64_t id[kInFlight];
@@ -70,14 +43,14 @@ __global__ __launch_bounds__(kEmThreads) void embedding_kernel(const T *__restri
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) x[u][e] = 0.0f;
                 if (id[u] >= 0 && id[u] < V) {
-                    em_load<T, VEC>(table + id[u] * N + c, x[u]);
+                    load_vec<T, VEC>(table + id[u] * N + c, x[u]);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) x[u][e] *= scale;
                 }
             }
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u)
-                if (i0 + u * kPerBlock < n) em_store<T, VEC, PAST>(out + (i0 + u * kPerBlock) * N + c, x[u]);
+                if (i0 + u * kPerBlock < n) store_vec<T, VEC, PAST>(out + (i0 + u * kPerBlock) * N + c, x[u]);
         }
     }
 }
@@ -124,7 +97,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortSource s, 
     const int n_bins = 1 << bits;
     for (int i = threadIdx.x; i < n_bins; i += kSortThreads) bins[i] = 0;
     __syncthreads();
-    const int64_t there = FIRST ? em_rows_there(s.offsets, s.B, s.rows) : 0;
+    const int64_t there = FIRST ? rows_there(s.offsets, s.B, s.rows) : 0;
     const int first = (int)blockIdx.x * kEmTile, end = s.rows - first < kEmTile ? s.rows : first + kEmTile;
     for (int i = first + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&bins[(sort_key<FIRST>(s, there, i) >> shift) & (n_bins - 1)], 1u);
     __syncthreads();
@@ -174,7 +147,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, 
     if ((int)blockIdx.x >= tiles) return clear_share(clearing, clearing.from + blockIdx.x - tiles);
     const int n_bins = 1 << bits, mask = n_bins - 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t there = FIRST ? em_rows_there(s.offsets, s.B, s.rows) : 0;
+    const int64_t there = FIRST ? rows_there(s.offsets, s.B, s.rows) : 0;
     for (int i = threadIdx.x; i < n_bins * kWaves; i += kSortThreads) next[i >> bits][i & mask] = 0;
     const int first = (int)blockIdx.x * kEmTile + wave * kMine;
     uint32_t key[kRounds];
@@ -257,7 +230,7 @@ template <typename T, int VEC, int LANES>
 __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restrict__ dout, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ positions, int rows,
                                                                 int n_blocks, uint32_t V, int64_t N, float scale, T *__restrict__ dtable, float *__restrict__ heads,
                                                                 float *__restrict__ tails) {
-    typedef typename EmVec<T, VEC>::Type Raw;
+    typedef typename RowVec<T, VEC>::Type Raw;
     constexpr int kAhead = 8;
     const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
     if (k >= n_blocks) return;
@@ -270,7 +243,7 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
     for (int i = 0; i < kEach; ++i) {
         const int r = first + i * LANES + lane < end ? first + i * LANES + lane : end - 1;
         my_key[i] = keys[r];
-        my_position[i] = positions[r];
+        my_position[i] = my_key[i] < V ? positions[r] : ~0u;   // a row that nobody adds (it may not be there) is not read
     }
     const auto of = [&](const uint32_t (&x)[kEach], int r) { return (uint32_t)__shfl((int)x[r / LANES], r % LANES, LANES); };   // r: a constant
     for (int64_t c = lane * VEC; c - lane * VEC < N; c += LANES * VEC) {   // (every lane takes part in the exchanges)
@@ -280,7 +253,7 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const uint32_t at = of(my_position, from + u);
-                if (mine) row[buffer][u] = *reinterpret_cast<const Raw *>(dout + (int64_t)at * N + c);
+                row[buffer][u] = mine && at != ~0u ? *reinterpret_cast<const Raw *>(dout + (int64_t)at * N + c) : Raw{};
             }
         };
         float sum[VEC];
@@ -290,11 +263,11 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
         auto row_is_done = [&]() {
             if (!mine) return;
-            if (!began) em_store<float, VEC>(heads + (int64_t)k * N + c, sum);
+            if (!began) store_vec<float, VEC>(heads + (int64_t)k * N + c, sum);
             else if (current < V) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-                em_store<T, VEC>(dtable + (int64_t)current * N + c, sum);
+                store_vec<T, VEC>(dtable + (int64_t)current * N + c, sum);
             }
         };
         read(0, 0);
@@ -322,7 +295,7 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
             }
         }
         if (!began || current != after) row_is_done();
-        else if (mine) em_store<float, VEC>(tails + (int64_t)k * N + c, sum);
+        else if (mine) store_vec<float, VEC>(tails + (int64_t)k * N + c, sum);
     }
 }
 
@@ -333,7 +306,7 @@ template <int VEC> __device__ inline void add_rows(const float *src, int64_t N, 
         float x[kAhead][VEC];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (r + u < to) em_load<float, VEC>(src + (int64_t)(r + u) * N + c, x[u]);
+            if (r + u < to) load_vec<float, VEC>(src + (int64_t)(r + u) * N + c, x[u]);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
             if (r + u < to) {
@@ -371,7 +344,7 @@ __global__ __launch_bounds__(kEmThreads) void super_sums_kernel(const uint32_t *
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
         if (c < N && group * kEach < kEmSuper) add_rows<VEC>(heads, N, c, k * kEmSuper + group * kEach, k * kEmSuper + (group + 1) * kEach, sum);
         groups_sum<VEC, LANES>(sum, slots);
-        if (group == 0 && c < N) em_store<float, VEC>(supers + (int64_t)k * N + c, sum);
+        if (group == 0 && c < N) store_vec<float, VEC>(supers + (int64_t)k * N + c, sum);
     }
 }
 
@@ -415,11 +388,11 @@ __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t 
     if (key < V && !many)
         for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
             float sum[VEC];
-            em_load<float, VEC>(tails + (int64_t)k * N + c, sum);
+            load_vec<float, VEC>(tails + (int64_t)k * N + c, sum);
             add_rows<VEC>(heads, N, c, k + 1, last + 1, sum);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-            em_store<T, VEC>(dtable + (int64_t)key * N + c, sum);
+            store_vec<T, VEC>(dtable + (int64_t)key * N + c, sum);
         }
     for (int g = 0; g < kPer; ++g) {
         const int b = long_block[g], end = long_last[g];
@@ -438,7 +411,7 @@ __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t 
                     const int each = (to - from + kPer - 1) / kPer, mine = from + group * each;
                     add_rows<VEC>(src, N, c, mine, mine + each < to ? mine + each : to, sum);
                 };
-                if (group == 0) em_load<float, VEC>(tails + (int64_t)b * N + c, sum);
+                if (group == 0) load_vec<float, VEC>(tails + (int64_t)b * N + c, sum);
                 part(heads, b + 1, head1);
                 if (any) {
                     part(supers, super0, super1);
@@ -449,7 +422,7 @@ __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t 
             if (group == 0 && c < N) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-                em_store<T, VEC>(dtable + (int64_t)id * N + c, sum);
+                store_vec<T, VEC>(dtable + (int64_t)id * N + c, sum);
             }
         }
     }

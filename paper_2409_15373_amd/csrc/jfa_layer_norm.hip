@@ -5,35 +5,13 @@
 // mean, the variance about it and the result, in fp32.  A row has a wave while N is at most kWaveMost vectors, a workgroup beyond; rows
 // too long for registers are read again from the caches.  dw and db are summed where a row passes through: a lane has the same columns of
 // every row that its wave takes, so its sums are registers until the end, one partial row per workgroup; a second launch adds those in a fixed order.
-#include "jfa_common.h"
-#include "jfa_mfma.h"
+#include "jfa_rows.h"
 
 namespace jfa {
 
 namespace {
 
 constexpr int kLnThreads = 256;
-
-template <typename T, int VEC> struct Vec { typedef T Type __attribute__((ext_vector_type(VEC))); };
-template <typename T> struct Vec<T, 1> { typedef T Type; };
-
-template <typename T, int VEC> __device__ inline void load_vec(const T *p, float (&x)[VEC]) {
-    const typename Vec<T, VEC>::Type v = *reinterpret_cast<const typename Vec<T, VEC>::Type *>(p);
-    if constexpr (VEC == 1) x[0] = (float)v;
-    else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[e] = (float)v[e];
-    }
-}
-template <typename T, int VEC> __device__ inline void store_vec(T *p, const float (&x)[VEC]) {
-    typename Vec<T, VEC>::Type v;
-    if constexpr (VEC == 1) v = (T)x[0];
-    else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = (T)x[e];
-    }
-    *reinterpret_cast<typename Vec<T, VEC>::Type *>(p) = v;
-}
 
 // Sum over the `LANES` lanes that share a row (a power of two up to 64).
 template <int LANES> __device__ inline float lanes_sum(float x) {
@@ -50,23 +28,13 @@ __device__ inline float block_sum(float x, float *slots) {
     return (slots[0] + slots[1]) + (slots[2] + slots[3]);
 }
 
-// Rows of the jagged tensor that there are: offsets[B], if given, at most the buffer's.
-__device__ inline int64_t rows_there(const int64_t *offsets, int64_t B, int64_t rows, int64_t reps) {
-    int64_t n = rows;
-    if (offsets) {
-        const int64_t have = offsets[B];
-        n = have < 0 ? 0 : have < rows ? have : rows;
-    }
-    return n * reps;
-}
-
 // LANES lanes per row (a wave or part of one), ITEMS vectors of VEC elements each.
 template <typename T, int VEC, int ITEMS, int LANES>
 __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(const T *__restrict__ x, const T *__restrict__ weight, const T *__restrict__ bias,
                                                                 const int64_t *__restrict__ offsets, int64_t B, int64_t rows, int64_t reps, int N, float eps,
                                                                 T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd) {
     constexpr int kPerBlock = kLnThreads / LANES;
-    const int64_t n = rows_there(offsets, B, rows, reps);
+    const int64_t n = rows_there(offsets, B, rows) * reps;
     const int lane = threadIdx.x % LANES;
     const float inv = 1.0f / (float)N;
     for (int64_t r = (int64_t)blockIdx.x * kPerBlock + threadIdx.x / LANES; r < n; r += (int64_t)gridDim.x * kPerBlock) {
@@ -117,7 +85,7 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_long_kernel(const T *__
                                                                      const int64_t *__restrict__ offsets, int64_t B, int64_t rows, int64_t reps, int64_t N,
                                                                      float eps, T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd) {
     __shared__ float slots[4];
-    const int64_t n = rows_there(offsets, B, rows, reps);
+    const int64_t n = rows_there(offsets, B, rows) * reps;
     const float inv = 1.0f / (float)N;
     for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const T *row = x + r * N;
@@ -160,7 +128,7 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_backward_kernel(const T
                                                                          T *__restrict__ dx, float *__restrict__ partial) {
     constexpr int kPerBlock = kLnThreads / LANES, kCols = ITEMS * VEC * LANES;
     __shared__ float sums[4][kCols];   // of each wave
-    const int64_t n = rows_there(offsets, B, rows, reps);
+    const int64_t n = rows_there(offsets, B, rows) * reps;
     const int lane = threadIdx.x % LANES, wave = threadIdx.x >> 6;
     const float inv = 1.0f / (float)N;
     float dw[ITEMS][VEC], db[ITEMS][VEC];
@@ -235,7 +203,7 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_backward_long_kernel(co
                                                                               const int64_t *__restrict__ offsets, int64_t B, int64_t rows, int64_t reps,
                                                                               int64_t N, T *__restrict__ dx) {
     __shared__ float slots[4];
-    const int64_t n = rows_there(offsets, B, rows, reps);
+    const int64_t n = rows_there(offsets, B, rows) * reps;
     const float inv = 1.0f / (float)N;
     for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const float m = mean[r], rs = rstd[r];
@@ -271,7 +239,7 @@ template <typename T>
 __global__ __launch_bounds__(kLnThreads) void layer_norm_columns_kernel(const T *__restrict__ x, const T *__restrict__ dy, const float *__restrict__ mean,
                                                                         const float *__restrict__ rstd, const int64_t *__restrict__ offsets, int64_t B,
                                                                         int64_t rows, int64_t reps, int64_t N, float *__restrict__ partial) {
-    const int64_t n = rows_there(offsets, B, rows, reps), c = (int64_t)blockIdx.x * kLnThreads + threadIdx.x;
+    const int64_t n = rows_there(offsets, B, rows) * reps, c = (int64_t)blockIdx.x * kLnThreads + threadIdx.x;
     if (c >= N) return;
     float dw = 0.0f, db = 0.0f;
 #pragma unroll 4

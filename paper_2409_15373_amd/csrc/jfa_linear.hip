@@ -597,13 +597,13 @@ LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, b
     LinearPlan p;
     const int64_t W = (int64_t)((double)rows * H / kPlaces);
     p.segments = 1;
-    p.segment_rows = max_len;
+    p.segment_rows = max_len > 0 ? max_len : 1;
     p.between = 0;
     if (max_len > rows) max_len = rows;
     if (max_len > 640 + 3.3 * W) {
         int64_t segment = (W + 63) / 64 * 64;
         segment = segment < kLeastSegment ? kLeastSegment : segment > kMostSegment ? kMostSegment : segment;
-        if (segment < max_len) {
+        if (segment < max_len && B * H * ((max_len + segment - 1) / segment) <= (int64_t)1 << 19) {   // (what the launches reach)
             p.segments = (int)((max_len + segment - 1) / segment);
             p.segment_rows = segment;
             p.between = (int)(rows / segment);
