@@ -129,24 +129,24 @@ __device__ inline int64_t state_between(int walk, int h, int H, int between, int
 // A workgroup takes one (sample, head, segment), blockIdx.x, through ROLES walks that go the same way over the same tensors: one of them (walk
 // blockIdx.y), or the two that give dk and dv, which share the tiles of q and dout.  Each walk has D / 32 waves, each of which owns 32 columns of
 // the state and of the outputs.
-// fp32, D = 64 and 128, one walk: twice as many, two to a strip of 32 columns with half of the state's rows each (linear_parts): the fp32 matrix instructions are what
-// a chunk waits for (64 clocks for 4096 products), and this way a wave has 48 of them instead of 112 in a chunk (D = 64; D = 128: 80 of 208).  P is summed over its
-// contraction, a step of 16 for each wave, and out over the two halves, through LDS.  (A sample of 256 rows, D = 64, 34 -> 25 us.  Two walks: there 8 waves a compute
-// unit have both forms' room, and 2048 of 256 rows took 443 us for all gradients, 409 without.)
+// KS = 2 (one walk; D = 64, and fp32 at D = 128): twice as many waves, two to a strip of 32 columns with half of the state's rows each; out is summed over
+// the two halves through LDS.  Where few walks run, what a chunk takes is the issue of one wave's instructions.  fp32: the fp32 matrix instructions,
+// 64 clocks for 4096 products, are what a chunk waits for: 48 of them for a wave instead of 112 (D = 128: 80 of 208); there P, too, is a sum over the waves, a
+// contraction step of 16 of each (a sample of 256 rows, D = 64, 34 -> 25 us).  bf16, D = 64: 16 samples of 600 rows 28.8 -> 24.4 us, 1024 94.9 -> 78.6;
+// at D = 128 the four waves fill the SIMDs: 16 samples 34.8 and 34.3 us, 1024 158 and 177.
 // bf16: what is rounded in front of a product (P, the state as a factor of out, the decayed rows of C) is split into two bf16 numbers, 16 bits in
 // all, so that a result's error is its own rounding; kParts = 3, exact, for the decayed rows where the state is itself a result.  One bf16 number each
 // would be 1.65 times that error (root mean square), and at D = 128 save 6 % of the forward and 12 % of the backward (2048 samples of 600 rows 299 -> 280 us and
 // 848 -> 738), the state's alone half of both.
 // kStateOnly: the state that a segment adds to, for those with a segment after them, into `carried`.
-template <typename T, int D, int ROLES> __host__ __device__ constexpr int linear_parts() { return sizeof(T) == 4 && D > 32 && ROLES == 1 ? 2 : 1; }
-template <typename T, int D, int ROLES, int kParts, bool kStateOnly>
-__global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES == 1 ? 2 : 1), 2) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
+template <typename T, int D, int ROLES, int KS, int kParts, bool kStateOnly>
+__global__ __launch_bounds__(2 * D * ROLES * KS, 2) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
                                                                        const int32_t *__restrict__ order, int B, int H, int segments, int segment_rows, int between,
                                                                        float *__restrict__ carried) {
     typedef Elem<T> E;
     typedef typename E::Operand Operand;
     constexpr int kRows = E::kRows, kSize = (int)sizeof(T), kStateTiles = D / 32, kSteps = D / 16, kSplit = E::kSplit;
-    constexpr int KS = linear_parts<T, D, ROLES>(), kWalkWaves = kStateTiles * KS, kWaves = kWalkWaves * ROLES, kMine = kStateTiles / KS;   // kMine: state tiles of a wave
+    constexpr int kWalkWaves = kStateTiles * KS, kWaves = kWalkWaves * ROLES, kMine = kStateTiles / KS;   // kMine: state tiles of a wave
     constexpr int kTiles = kRows / 32, kPTiles = kTiles * (kTiles + 1) / 2;
     constexpr int kChunks = D * kSize / 16, kTileBytes = kRows * kChunks * 16, kLoads = kRows * kChunks / (64 * kWaves);   // 16-byte chunks of a row; copies of a tile per wave
     // Places of tiles.  A is free for the next chunk's once the state's product with it is done, in the middle of a chunk.  B and, of two walks, C (their B
@@ -157,8 +157,11 @@ __global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES 
     // one tile) has it in registers.
     constexpr bool kShareP = !kStateOnly && kPTiles > 1 && kStateTiles > 1;
     constexpr int kPBytes = kShareP ? kPTiles * 2 * kSplit * 1024 : 0;
-    static_assert(KS == 1 || (kTiles == 1 && kSteps == kWalkWaves), "a step of P's contraction for each wave");
-    constexpr int kXBytes = KS > 1 && !kStateOnly ? kWalkWaves * (4 + 2) * 1024 : 0;   // a wave's part of P, half of its part of out
+    constexpr bool kSumP = KS > 1 && kTiles == 1;
+    static_assert(KS == 1 || ROLES == 1, "");
+    static_assert(!kSumP || kSteps == kWalkWaves, "a step of P's contraction for each wave");
+    constexpr int kHalf = kTiles == 1 ? 2 : 4;   // kilobytes of the half of out that a wave gives away
+    constexpr int kXBytes = KS > 1 && !kStateOnly ? kWalkWaves * ((kSumP ? 4 : 0) + kHalf) * 1024 : 0;   // a wave's part of P, half of its part of out
     __shared__ __attribute__((aligned(16))) char lds[kPlaces * kTileBytes + ROLES * (kPBytes + kXBytes)];
     __shared__ float powers[ROLES][2][2 * kRows];
 
@@ -282,7 +285,7 @@ __global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES 
         const char *const at = lds + role * kTileBytes;
         const char *const bt = lds + (ROLES == 2 ? 2 + 2 * role + turn : 2 + turn) * kTileBytes, *const ct = lds + (ROLES == 2 ? 4 - 2 * role + turn : 1) * kTileBytes;
         char *const pt = lds + kPlaces * kTileBytes + role * kPBytes;
-        char *const px = lds + kPlaces * kTileBytes + role * kXBytes, *const ox = px + kWalkWaves * 4096;   // KS > 1
+        char *const px = lds + kPlaces * kTileBytes + ROLES * kPBytes, *const ox = px + (kSumP ? kWalkWaves * 4096 : 0);   // KS > 1
         Operand c[2 * kTiles];   // the chunk's rows of C, this wave's columns
         if (kStateOnly) {
             c_is_there();
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES 
         }
         if (!kStateOnly) {
             // P^T, tiles (rows j of B) x (columns i of A), zero above the diagonal
-            Operand P[kShareP || KS > 1 ? 1 : kPTiles][2][kSplit];
+            Operand P[kShareP || kSumP ? 1 : kPTiles][2][kSplit];
             const float *const near = my_powers[0] + kRows + col - 4 * half;   // [-(8 g + e)]: g^(i - j)
             auto weighted = [&](f32x16 &p, int t, auto &&put) {   // t: 0, 2 on the diagonal, 1 below it; put(contraction step, part, operand)
 #pragma unroll
@@ -310,7 +313,7 @@ __global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES 
                     }
                 }
             };
-            if constexpr (KS > 1) {
+            if constexpr (kSumP) {
                 f32x16 p;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) p[v] = 0.0f;
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES 
             } else if constexpr (kShareP) {
 #pragma unroll
                 for (int t = 0; t < kPTiles; ++t) {
-                    if (t % kStateTiles != strip) continue;
+                    if (t % kWalkWaves != walk_wave) continue;
                     // operands one step ahead of the products that use them: left alone, every read sits right in front of its product
                     Operand a[2], x[2];
                     auto read = [&](int ks) {
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES 
             for (int ti = 0; ti < kTiles; ++ti)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[ti][v] *= since[ti];
-            if constexpr (KS > 1) {
+            if constexpr (kSumP) {
                 // this wave's half of P's rows, summed over the waves, with the same rows of C; then its half of out's columns, summed over the two
                 f32x8 x;
 #pragma unroll
@@ -443,29 +446,50 @@ __global__ __launch_bounds__(2 * D * ROLES * (sizeof(T) == 4 && D > 32 && ROLES 
                     }
                 }
             } else {
+                // (KS = 2: every second step of P's rows, and one of the two tiles of out's rows)
+                const auto product_with_p = [&](int ks, const char *from) {
 #pragma unroll
-            for (int ks = 0; ks < 2 * kTiles; ++ks)
+                    for (int half_p = 0; half_p < kSplit; ++half_p) {
+                        const auto p = [&](int t) -> Operand {
+                            if constexpr (kShareP) return *reinterpret_cast<const Operand *>(from + ((t * 2 + (ks & 1)) * kSplit + half_p) * 1024 + lane * 16);
+                            else return P[t][ks & 1][half_p];
+                        };
+                        if (ks < 2) o[0] = E::product(c[ks], p(0), o[0]);
+                        if constexpr (kTiles == 2) o[1] = E::product(c[ks], p(ks < 2 ? 1 : 2), o[1]);
+                    }
+                };
 #pragma unroll
-                for (int part = 0; part < kSplit; ++part) {
-                    const auto p = [&](int t) -> Operand {
-                        if constexpr (kShareP) return *reinterpret_cast<const Operand *>(pt + ((t * 2 + (ks & 1)) * kSplit + part) * 1024 + lane * 16);
-                        else return P[t][ks & 1][part];
-                    };
-                    if (ks < 2) o[0] = E::product(c[ks], p(0), o[0]);
-                    if constexpr (kTiles == 2) o[1] = E::product(c[ks], p(ks < 2 ? 1 : 2), o[1]);
-                }
-            char *const out = reinterpret_cast<char *>((T *)walk.out + low);
+                for (int ks = 0; ks < 2 * kTiles; ++ks)
+                    if (KS == 1 || (ks & 1) == part) product_with_p(ks, pt);
+                char *const out = reinterpret_cast<char *>((T *)walk.out + low);
+                auto store = [&](int ti, const f32x16 &o) {
+                    const int r = ti * 32 + col;
+                    if (r < rows) {
+                        char *const dst = out + ((uint32_t)(reverse ? kRows - 1 - r : r) * row_bytes + (uint32_t)(strip * 32 + half * 4) * kSize);
 #pragma unroll
-            for (int ti = 0; ti < kTiles; ++ti) {
-                const int r = ti * 32 + col;
-                if (r < rows) {
-                    char *const dst = out + ((uint32_t)(reverse ? kRows - 1 - r : r) * row_bytes + (uint32_t)(strip * 32 + half * 4) * kSize);
+                        for (int g = 0; g < 4; ++g)
+                            E::store4(reinterpret_cast<T *>(dst + g * 8 * kSize), f32x4{o[4 * g] * out_scale, o[4 * g + 1] * out_scale, o[4 * g + 2] * out_scale, o[4 * g + 3] * out_scale});
+                    }
+                };
+                if constexpr (KS > 1) {
+                    f32x16 mine = part ? o[kTiles - 1] : o[0];
+                    const f32x16 others = part ? o[0] : o[kTiles - 1];
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
-                        E::store4(reinterpret_cast<T *>(dst + g * 8 * kSize),
-                                  f32x4{o[ti][4 * g] * out_scale, o[ti][4 * g + 1] * out_scale, o[ti][4 * g + 2] * out_scale, o[ti][4 * g + 3] * out_scale});
+                        *reinterpret_cast<f32x4 *>(ox + (walk_wave * 4 + g) * 1024 + lane * 16) = f32x4{others[4 * g], others[4 * g + 1], others[4 * g + 2], others[4 * g + 3]};
+                    __syncthreads();
+                    const int partner = strip + (1 - part) * kStateTiles;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 y = *reinterpret_cast<const f32x4 *>(ox + (partner * 4 + g) * 1024 + lane * 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mine[4 * g + e] += y[e];
+                    }
+                    store(part, mine);
+                } else {
+#pragma unroll
+                    for (int ti = 0; ti < kTiles; ++ti) store(ti, o[ti]);
                 }
-            }
             }
         }
         // S <- g^rows S + (g^(rows - 1 - i) B)^T C, unless nobody looks at it any more
@@ -616,33 +640,36 @@ LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, b
     return p;
 }
 
-template <typename T, int D, int kParts>
-static void launch_walks(const LinearWalks &walks, bool backward, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H, int segments,
-                         int segment_rows, int between, bool apart, float *carried, hipStream_t stream) {
+template <typename T, int D, int KS, int kParts>
+static void launch_walks(const LinearWalks &walks, bool backward, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H, const LinearPlan &p,
+                         float *carried, hipStream_t stream) {
+    const int segments = p.segments, segment_rows = (int)p.segment_rows, between = p.between;
     const unsigned blocks = (unsigned)((D * sizeof(T) < 128 ? (B * segments + 7) / 8 * 8 : B * segments) * H);
-    constexpr int kThreads = 2 * D * linear_parts<T, D, 1>();
+    constexpr int kThreads = 2 * D * KS;
     if (segments > 1) {   // walk 0, and of the two that go back, which have one state, walk 2
         const LinearWalks states{{walks.walk[0], walks.walk[2], walks.walk[2]}};
         const int n = backward ? 2 : 1;
-        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, true>), dim3(blocks, n), dim3(kThreads), 0, stream, states, log_decay, offsets, order, (int)B, H, segments, segment_rows,
-                           between, carried);
+        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, KS, kParts, true>), dim3(blocks, n), dim3(kThreads), 0, stream, states, log_decay, offsets, order, (int)B, H, segments,
+                           segment_rows, between, carried);
         hipLaunchKernelGGL(linear_carry_kernel, dim3((unsigned)(B * H * (D * D / 1024)), n), dim3(256), 0, stream, states, log_decay, offsets, H, D, segments, segment_rows,
                            between, carried);
     }
-    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, kParts, false>), dim3(blocks, backward && apart ? 3 : 1), dim3(kThreads), 0, stream, walks, log_decay, offsets, order, (int)B, H,
+    constexpr bool kTwo = sizeof(T) == 2 || D < 128;   // (fp32 at D = 128: two walks have no room on a compute unit)
+    const bool apart = p.apart || !kTwo;
+    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, KS, kParts, false>), dim3(blocks, backward && apart ? 3 : 1), dim3(kThreads), 0, stream, walks, log_decay, offsets, order, (int)B, H,
                        segments, segment_rows, between, carried);
-    if constexpr (sizeof(T) == 2 || D < 128)
+    if constexpr (kTwo)
         if (backward && !apart)
-            hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows,
+            hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, 1, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows,
                                between, carried);
 }
 template <typename T, int D>
 static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H,
                                const LinearPlan &p, float *carried, hipStream_t stream) {
-    const int segment_rows = (int)p.segment_rows;
-    if constexpr (sizeof(T) == 4) launch_walks<T, D, 1>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, p.apart || (sizeof(T) == 4 && D == 128), carried, stream);
-    else if (states) launch_walks<T, D, 3>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, p.apart || (sizeof(T) == 4 && D == 128), carried, stream);
-    else launch_walks<T, D, 2>(walks, backward, log_decay, offsets, order, B, H, p.segments, segment_rows, p.between, p.apart || (sizeof(T) == 4 && D == 128), carried, stream);
+    constexpr int KS = D == 64 || (D == 128 && sizeof(T) == 4) ? 2 : 1;
+    if constexpr (sizeof(T) == 4) launch_walks<T, D, KS, 1>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
+    else if (states) launch_walks<T, D, KS, 3>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
+    else launch_walks<T, D, KS, 2>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
     return hipGetLastError();
 }
 
