@@ -26,31 +26,32 @@ constexpr int kSortThreads = 1024;
 // what has more of them than the L2s hold: the table's frequent rows stay (131072 rows of 512, 37 -> 25 us).
 constexpr int kInFlight = 2;
 constexpr int64_t kL2Bytes = 32 << 20;
-template <typename T, typename Id, int VEC, int LANES, bool PAST>
+template <typename T, typename Id, bool EVEN, int LANES, bool PAST>
 __global__ __launch_bounds__(kEmThreads) void embedding_kernel(const T *__restrict__ table, const Id *__restrict__ ids, const int64_t *__restrict__ offsets,
                                                                int64_t B, int64_t rows, int64_t V, int64_t N, float scale, T *__restrict__ out) {
-    constexpr int kPerBlock = kEmThreads / LANES;
+    constexpr int kPerBlock = kEmThreads / LANES, VEC = kRowVec<T>;
     const int64_t n = rows_there(offsets, B, rows);
     const int lane = threadIdx.x % LANES;
     for (int64_t i0 = (int64_t)blockIdx.x * kPerBlock * kInFlight + threadIdx.x / LANES; i0 < n; i0 += (int64_t)gridDim.x * kPerBlock * kInFlight) {
         int64_t id[kInFlight];
 #pragma unroll
         for (int u = 0; u < kInFlight; ++u) id[u] = i0 + u * kPerBlock < n ? (int64_t)ids[i0 + u * kPerBlock] : -1;
-        for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
+        for (int64_t own = lane * VEC; own < N; own += LANES * VEC) {
+            const int64_t c = vec_at<VEC, EVEN>(own, N);
             float x[kInFlight][VEC];
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) x[u][e] = 0.0f;
                 if (id[u] >= 0 && id[u] < V) {
-                    load_vec<T, VEC>(table + id[u] * N + c, x[u]);
+                    load_vec<T, VEC, EVEN>(table + id[u] * N + c, N - c, x[u]);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) x[u][e] *= scale;
                 }
             }
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u)
-                if (i0 + u * kPerBlock < n) store_vec<T, VEC, PAST>(out + (i0 + u * kPerBlock) * N + c, x[u]);
+                if (i0 + u * kPerBlock < n) store_vec<T, VEC, EVEN, PAST>(out + (i0 + u * kPerBlock) * N + c, N - c, x[u]);
         }
     }
 }
@@ -226,12 +227,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, 
 // ---- sums of rows ----
 // Block k: sorted positions kEmBlock k up to the next block's (or the end).  An id whose positions are all inside: its row of the table.  The sum of those that
 // an earlier block's last id has in this one: heads[k]; of those of the last id, where it begins in this block and goes on in the next: tails[k].
-template <typename T, int VEC, int LANES>
+template <typename T, bool EVEN, int LANES>
 __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restrict__ dout, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ positions, int rows,
                                                                 int n_blocks, uint32_t V, int64_t N, float scale, T *__restrict__ dtable, float *__restrict__ heads,
                                                                 float *__restrict__ tails) {
-    typedef typename RowVec<T, VEC>::Type Raw;
-    constexpr int kAhead = 8;
+    constexpr int kAhead = 8, VEC = kRowVec<T>;
+    typedef RowRaw<T, VEC> Raw;
     const int k = blockIdx.x * (kEmThreads / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
     if (k >= n_blocks) return;
     const int first = k * kEmBlock, end = rows - first < kEmBlock ? rows : first + kEmBlock;
@@ -246,14 +247,15 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
         my_position[i] = my_key[i] < V ? positions[r] : ~0u;   // a row that nobody adds (it may not be there) is not read
     }
     const auto of = [&](const uint32_t (&x)[kEach], int r) { return (uint32_t)__shfl((int)x[r / LANES], r % LANES, LANES); };   // r: a constant
-    for (int64_t c = lane * VEC; c - lane * VEC < N; c += LANES * VEC) {   // (every lane takes part in the exchanges)
-        const bool mine = c < N;
+    for (int64_t own = lane * VEC; own - lane * VEC < N; own += LANES * VEC) {   // (every lane takes part in the exchanges)
+        const bool mine = own < N;
+        const int64_t c = vec_at<VEC, EVEN>(own, N);
         Raw row[2][kAhead];
         auto read = [&](int from, int buffer) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const uint32_t at = of(my_position, from + u);
-                row[buffer][u] = mine && at != ~0u ? *reinterpret_cast<const Raw *>(dout + (int64_t)at * N + c) : Raw{};
+                row[buffer][u] = mine && at != ~0u ? read_vec<T, VEC, EVEN>(dout + (int64_t)at * N + c, N - c) : Raw{};
             }
         };
         float sum[VEC];
@@ -263,11 +265,11 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
         auto row_is_done = [&]() {
             if (!mine) return;
-            if (!began) store_vec<float, VEC>(heads + (int64_t)k * N + c, sum);
+            if (!began) store_vec<float, VEC, EVEN>(heads + (int64_t)k * N + c, N - c, sum);
             else if (current < V) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-                store_vec<T, VEC>(dtable + (int64_t)current * N + c, sum);
+                store_vec<T, VEC, EVEN>(dtable + (int64_t)current * N + c, N - c, sum);
             }
         };
         read(0, 0);
@@ -287,26 +289,23 @@ __global__ __launch_bounds__(kEmThreads) void block_sums_kernel(const T *__restr
                     for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
                 }
                 const Raw x = row[batch & 1][u];
-                if constexpr (VEC == 1) sum[0] += (float)x;
-                else {
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) sum[e] += (float)x[e];
-                }
+                for (int e = 0; e < VEC; ++e) sum[e] += (float)x[e];
             }
         }
         if (!began || current != after) row_is_done();
-        else if (mine) store_vec<float, VEC>(tails + (int64_t)k * N + c, sum);
+        else if (mine) store_vec<float, VEC, EVEN>(tails + (int64_t)k * N + c, N - c, sum);
     }
 }
 
 // Adds rows from .. to - 1 of `src`, kAhead loads in flight.
-template <int VEC> __device__ inline void add_rows(const float *src, int64_t N, int64_t c, int from, int to, float (&sum)[VEC]) {
+template <int VEC, bool EVEN> __device__ inline void add_rows(const float *src, int64_t N, int64_t c, int from, int to, float (&sum)[VEC]) {
     constexpr int kAhead = 8;
     for (int r = from; r < to; r += kAhead) {
         float x[kAhead][VEC];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (r + u < to) load_vec<float, VEC>(src + (int64_t)(r + u) * N + c, x[u]);
+            if (r + u < to) load_vec<float, VEC, EVEN>(src + (int64_t)(r + u) * N + c, N - c, x[u]);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
             if (r + u < to) {
@@ -329,7 +328,7 @@ template <int VEC, int LANES> __device__ inline void groups_sum(float (&sum)[VEC
 }
 
 // supers[k]: the sum of heads kEmSuper k .. kEmSuper (k + 1) - 1, where one id has all of their positions and began earlier.  A workgroup each.
-template <int VEC, int LANES>
+template <int VEC, bool EVEN, int LANES>
 __global__ __launch_bounds__(kEmThreads) void super_sums_kernel(const uint32_t *__restrict__ keys, uint32_t V, int64_t N, const float *__restrict__ heads,
                                                                 float *__restrict__ supers) {
     constexpr int kPer = kEmThreads / LANES, kEach = kEmSuper > kPer ? kEmSuper / kPer : 1;   // heads of a lane group
@@ -338,23 +337,24 @@ __global__ __launch_bounds__(kEmThreads) void super_sums_kernel(const uint32_t *
     const int64_t first = (int64_t)k * kEmSuper * kEmBlock;
     const uint32_t key = keys[first];
     if (key >= V || keys[first + kEmSuper * kEmBlock - 1] != key || first == 0 || keys[first - 1] != key) return;
-    for (int64_t c = lane * VEC; c - lane * VEC < N; c += LANES * VEC) {
+    for (int64_t own = lane * VEC; own - lane * VEC < N; own += LANES * VEC) {
+        const int64_t c = vec_at<VEC, EVEN>(own, N);
         float sum[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-        if (c < N && group * kEach < kEmSuper) add_rows<VEC>(heads, N, c, k * kEmSuper + group * kEach, k * kEmSuper + (group + 1) * kEach, sum);
+        if (own < N && group * kEach < kEmSuper) add_rows<VEC, EVEN>(heads, N, c, k * kEmSuper + group * kEach, k * kEmSuper + (group + 1) * kEach, sum);
         groups_sum<VEC, LANES>(sum, slots);
-        if (group == 0 && c < N) store_vec<float, VEC>(supers + (int64_t)k * N + c, sum);
+        if (group == 0 && own < N) store_vec<float, VEC, EVEN>(supers + (int64_t)k * N + c, N - c, sum);
     }
 }
 
 // The rows of ids that begin in one block and end in another.  A workgroup has a block for each of its groups of LANES lanes; ids with more
 // than kFewHeads heads are added by all of them together.
-template <typename T, int VEC, int LANES>
+template <typename T, bool EVEN, int LANES>
 __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t *__restrict__ keys, int n_blocks, uint32_t V, int64_t N, float scale,
                                                                  const float *__restrict__ heads, const float *__restrict__ tails, const float *__restrict__ supers,
                                                                  T *__restrict__ dtable) {
-    constexpr int kPer = kEmThreads / LANES, kFewHeads = 16;
+    constexpr int kPer = kEmThreads / LANES, kFewHeads = 16, VEC = kRowVec<T>;
     __shared__ float slots[kEmThreads][VEC];
     __shared__ int long_block[kPer], long_last[kPer];
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, k = blockIdx.x * kPer + group;
@@ -386,13 +386,14 @@ __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t 
     }
     __syncthreads();
     if (key < V && !many)
-        for (int64_t c = lane * VEC; c < N; c += LANES * VEC) {
+        for (int64_t own = lane * VEC; own < N; own += LANES * VEC) {
+            const int64_t c = vec_at<VEC, EVEN>(own, N);
             float sum[VEC];
-            load_vec<float, VEC>(tails + (int64_t)k * N + c, sum);
-            add_rows<VEC>(heads, N, c, k + 1, last + 1, sum);
+            load_vec<float, VEC, EVEN>(tails + (int64_t)k * N + c, N - c, sum);
+            add_rows<VEC, EVEN>(heads, N, c, k + 1, last + 1, sum);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-            store_vec<T, VEC>(dtable + (int64_t)key * N + c, sum);
+            store_vec<T, VEC, EVEN>(dtable + (int64_t)key * N + c, N - c, sum);
         }
     for (int g = 0; g < kPer; ++g) {
         const int b = long_block[g], end = long_last[g];
@@ -402,16 +403,17 @@ __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t 
         const bool any = super0 < super1;
         const int head1 = any ? super0 * kEmSuper : end + 1;   // heads b + 1 .. head1 - 1, then supers, then heads super1 * kEmSuper .. end
         const uint32_t id = keys[(int64_t)(b + 1) * kEmBlock];
-        for (int64_t c = lane * VEC; c - lane * VEC < N; c += LANES * VEC) {
+        for (int64_t own = lane * VEC; own - lane * VEC < N; own += LANES * VEC) {
+            const int64_t c = vec_at<VEC, EVEN>(own, N);
             float sum[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-            if (c < N) {
+            if (own < N) {
                 const auto part = [&](const float *src, int from, int to) {   // this group's
                     const int each = (to - from + kPer - 1) / kPer, mine = from + group * each;
-                    add_rows<VEC>(src, N, c, mine, mine + each < to ? mine + each : to, sum);
+                    add_rows<VEC, EVEN>(src, N, c, mine, mine + each < to ? mine + each : to, sum);
                 };
-                if (group == 0) load_vec<float, VEC>(tails + (int64_t)b * N + c, sum);
+                if (group == 0) load_vec<float, VEC, EVEN>(tails + (int64_t)b * N + c, N - c, sum);
                 part(heads, b + 1, head1);
                 if (any) {
                     part(supers, super0, super1);
@@ -419,40 +421,40 @@ __global__ __launch_bounds__(kEmThreads) void join_blocks_kernel(const uint32_t 
                 }
             }
             groups_sum<VEC, LANES>(sum, slots);
-            if (group == 0 && c < N) {
+            if (group == 0 && own < N) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[e] *= scale;
-                store_vec<T, VEC>(dtable + (int64_t)id * N + c, sum);
+                store_vec<T, VEC, EVEN>(dtable + (int64_t)id * N + c, N - c, sum);
             }
         }
     }
 }
 
 template <typename T, typename Launch> hipError_t em_spread(int64_t N, bool aligned, Launch launch) {
-    constexpr int kVec = 16 / (int)sizeof(T);
-    const auto with = [&](auto vec) {
-        constexpr int V = decltype(vec)::value;
-        const int64_t vectors = (N + V - 1) / V;
+    constexpr int kVec = kRowVec<T>;
+    const auto with = [&](auto even) {
+        const int64_t vectors = (N + kVec - 1) / kVec;
         using std::integral_constant;
-        if (vectors <= 4) return launch(vec, integral_constant<int, 4>{});
-        if (vectors <= 8) return launch(vec, integral_constant<int, 8>{});
-        if (vectors <= 16) return launch(vec, integral_constant<int, 16>{});
-        if (vectors <= 32) return launch(vec, integral_constant<int, 32>{});
-        return launch(vec, integral_constant<int, 64>{});
+        if (vectors <= 4) return launch(even, integral_constant<int, 4>{});
+        if (vectors <= 8) return launch(even, integral_constant<int, 8>{});
+        if (vectors <= 16) return launch(even, integral_constant<int, 16>{});
+        if (vectors <= 32) return launch(even, integral_constant<int, 32>{});
+        return launch(even, integral_constant<int, 64>{});
     };
-    return aligned && N % kVec == 0 ? with(std::integral_constant<int, kVec>{}) : with(std::integral_constant<int, 1>{});
+    return aligned && N % kVec == 0 ? with(std::true_type{}) : with(std::false_type{});
 }
 
 template <typename T, typename Id>
 hipError_t embedding_t(const T *table, const Id *ids, const int64_t *offsets, int64_t B, int64_t rows, int64_t V, int64_t N, float scale, T *out, hipStream_t stream) {
-    return em_spread<T>(N, aligned16(table, out), [&](auto vec, auto lanes) {
-        constexpr int VEC = decltype(vec)::value, L = decltype(lanes)::value, kRows = kEmThreads / L * kInFlight;
+    return em_spread<T>(N, aligned16(table, out), [&](auto even, auto lanes) {
+        constexpr bool EVEN = decltype(even)::value;
+        constexpr int L = decltype(lanes)::value, kRows = kEmThreads / L * kInFlight;
         const int64_t need = (rows + kRows - 1) / kRows;
         const dim3 grid((unsigned)(need < 16384 ? need : 16384)), threads(kEmThreads);
         if (rows * N * (int64_t)sizeof(T) > kL2Bytes)
-            hipLaunchKernelGGL((embedding_kernel<T, Id, VEC, L, true>), grid, threads, 0, stream, table, ids, offsets, B, rows, V, N, scale, out);
+            hipLaunchKernelGGL((embedding_kernel<T, Id, EVEN, L, true>), grid, threads, 0, stream, table, ids, offsets, B, rows, V, N, scale, out);
         else
-            hipLaunchKernelGGL((embedding_kernel<T, Id, VEC, L, false>), grid, threads, 0, stream, table, ids, offsets, B, rows, V, N, scale, out);
+            hipLaunchKernelGGL((embedding_kernel<T, Id, EVEN, L, false>), grid, threads, 0, stream, table, ids, offsets, B, rows, V, N, scale, out);
         return hipGetLastError();
     });
 }
@@ -526,14 +528,15 @@ hipError_t embedding_backward_t(const T *dout, const void *ids, bool ids64, cons
         s.positions = positions;
     }
     float *const heads = reinterpret_cast<float *>(ws + p.heads), *const tails = reinterpret_cast<float *>(ws + p.tails), *const supers = reinterpret_cast<float *>(ws + p.supers);
-    return em_spread<T>(N, aligned16(dout, dtable), [&](auto vec, auto lanes) {
-        constexpr int VEC = decltype(vec)::value, L = decltype(lanes)::value, kPer = kEmThreads / L;
+    return em_spread<T>(N, aligned16(dout, dtable), [&](auto even, auto lanes) {
+        constexpr bool EVEN = decltype(even)::value;
+        constexpr int L = decltype(lanes)::value, kPer = kEmThreads / L;
         const dim3 blocks((p.n_blocks + kPer - 1) / kPer), few(kEmThreads);
-        hipLaunchKernelGGL((block_sums_kernel<T, VEC, L>), blocks, few, 0, stream, dout, s.keys, s.positions, (int)rows, p.n_blocks, (uint32_t)V, N, scale, dtable, heads, tails);
+        hipLaunchKernelGGL((block_sums_kernel<T, EVEN, L>), blocks, few, 0, stream, dout, s.keys, s.positions, (int)rows, p.n_blocks, (uint32_t)V, N, scale, dtable, heads, tails);
         if (p.n_supers)
-            hipLaunchKernelGGL((super_sums_kernel<VEC, L>), dim3(p.n_supers), few, 0, stream, s.keys, (uint32_t)V, N, heads, supers);
+            hipLaunchKernelGGL((super_sums_kernel<kRowVec<T>, EVEN, L>), dim3(p.n_supers), few, 0, stream, s.keys, (uint32_t)V, N, heads, supers);
         if (p.n_blocks > 1)
-            hipLaunchKernelGGL((join_blocks_kernel<T, VEC, L>), blocks, few, 0, stream, s.keys, p.n_blocks, (uint32_t)V, N, scale, heads, tails, supers, dtable);
+            hipLaunchKernelGGL((join_blocks_kernel<T, EVEN, L>), blocks, few, 0, stream, s.keys, p.n_blocks, (uint32_t)V, N, scale, heads, tails, supers, dtable);
         return hipGetLastError();
     });
 }
