@@ -3,7 +3,7 @@
 //   dx = rstd (w dy - mean(w dy) - xh mean(w dy xh));  dw = sum over rows of dy xh,  db = sum over rows of dy
 // Bound by HBM: x in and y out, and x and dy in and dx out.  A row is read once: it stays in the registers of the lanes that share it for the
 // mean, the variance about it and the result, in fp32.  A row has a wave or a part of one, or a workgroup; rows
-// too long for registers are read again from the caches.  dw and db are summed where a row passes through: a lane has the same columns of
+// too long for registers (more than 16 KB) are read again from the caches.  dw and db are summed where a row passes through: a lane has the same columns of
 // every row that its wave takes, so its sums are registers until the end, one partial row per workgroup; a second launch adds those in a fixed order.
 #include "jfa_rows.h"
 
@@ -40,52 +40,62 @@ template <typename T, int ITEMS, int LANES, bool EVEN> struct RowPart {
     }
 };
 
-// LANES lanes per row (a wave or part of one, or the workgroup), ITEMS vectors each.
+// Rows of the forward that are in flight at a time: two where the lanes of a row have few vectors of it (512 bf16 a row 4.9 -> 5.0 TB/s, 257 fp32 3.4 -> 4.0, 129
+// bf16 2.2 -> 2.6).  The backward's two tensors are enough (5.2 to 5.4 TB/s at 128 to 4096 bf16 a row; reading the next row ahead: 4.4 to 5.0 up to 1024).
+template <int ITEMS> constexpr int ln_rows = ITEMS <= 2 ? 2 : 1;
+
+// LANES lanes per row (a wave or part of one, or the workgroup), ITEMS vectors each, ln_rows rows at a time.
 template <typename T, int ITEMS, int LANES, bool EVEN>
 __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(const T *__restrict__ x, const T *__restrict__ weight, const T *__restrict__ bias,
                                                                 const int64_t *__restrict__ offsets, int64_t B, int64_t rows, int64_t reps, int N, float eps,
                                                                 T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd) {
-    constexpr int kPerBlock = kLnThreads / LANES, VEC = kRowVec<T>;
+    constexpr int kPerBlock = kLnThreads / LANES, VEC = kRowVec<T>, kRows = ln_rows<ITEMS>;
     __shared__ float slots[4];
-    const int64_t n = rows_there(offsets, B, rows) * reps, step = (int64_t)gridDim.x * kPerBlock;
+    const int64_t n = rows_there(offsets, B, rows) * reps, step = (int64_t)gridDim.x * kPerBlock * kRows;
     const int lane = threadIdx.x % LANES;
     const float inv = 1.0f / (float)N;
-    RowPart<T, ITEMS, LANES, EVEN> part;
-    for (int64_t r = (int64_t)blockIdx.x * kPerBlock + threadIdx.x / LANES; r < n; r += step) {
-        part.read(x, r, N, lane);
-        float v[ITEMS][VEC], sum = 0.0f;
+    for (int64_t r0 = (int64_t)blockIdx.x * kPerBlock * kRows + threadIdx.x / LANES; r0 < n; r0 += step) {
+        RowPart<T, ITEMS, LANES, EVEN> part[kRows];
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
-            widen_vec<T, VEC>(part.v[i], v[i]);
+        for (int u = 0; u < kRows; ++u) part[u].read(x, r0 + u * kPerBlock < n ? r0 + u * kPerBlock : r0, N, lane);   // (the first again behind the last row)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (EVEN || c + e >= own) sum += v[i][e];
-        }
-        const float m = lanes_sum<LANES>(sum, slots) * inv;
-        float square = 0.0f;
+        for (int u = 0; u < kRows; ++u) {
+            const int64_t r = r0 + u * kPerBlock;
+            float v[ITEMS][VEC], sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
+            for (int i = 0; i < ITEMS; ++i) {
+                const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
+                widen_vec<T, VEC>(part[u].v[i], v[i]);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (own < N && (EVEN || (c + e >= own && c + e < N))) square += (v[i][e] - m) * (v[i][e] - m);
-        }
-        const float rs = 1.0f / sqrtf(lanes_sum<LANES>(square, slots) * inv + eps);
-        if (lane == 0) {
-            if (mean) mean[r] = m;
-            if (rstd) rstd[r] = rs;
-        }
+                for (int e = 0; e < VEC; ++e)
+                    if (EVEN || c + e >= own) sum += v[i][e];
+            }
+            const float m = lanes_sum<LANES>(sum, slots) * inv;
+            float square = 0.0f;
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
-            if (own < N) {
-                float w[VEC], b[VEC];
-                if (weight) load_vec<T, VEC, EVEN>(weight + c, N - c, w);
-                if (bias) load_vec<T, VEC, EVEN>(bias + c, N - c, b);
+            for (int i = 0; i < ITEMS; ++i) {
+                const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) v[i][e] = (v[i][e] - m) * rs * (weight ? w[e] : 1.0f) + (bias ? b[e] : 0.0f);
-                store_vec<T, VEC, EVEN>(y + r * N + c, N - c, v[i]);
+                for (int e = 0; e < VEC; ++e)
+                    if (own < N && (EVEN || (c + e >= own && c + e < N))) square += (v[i][e] - m) * (v[i][e] - m);
+            }
+            const float rs = 1.0f / sqrtf(lanes_sum<LANES>(square, slots) * inv + eps);
+            if (kRows > 1 && r >= n) break;
+            if (lane == 0) {
+                if (mean) mean[r] = m;
+                if (rstd) rstd[r] = rs;
+            }
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
+                if (own < N) {
+                    float w[VEC], b[VEC];
+                    if (weight) load_vec<T, VEC, EVEN>(weight + c, N - c, w);
+                    if (bias) load_vec<T, VEC, EVEN>(bias + c, N - c, b);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[i][e] = (v[i][e] - m) * rs * (weight ? w[e] : 1.0f) + (bias ? b[e] : 0.0f);
+                    store_vec<T, VEC, EVEN>(y + r * N + c, N - c, v[i]);
+                }
             }
         }
     }
@@ -316,7 +326,8 @@ int64_t ln_grid(int64_t rows, int per_block) {
 }
 
 // How a row of N elements of T is spread: up to a wave's lanes with a vector each, then up to four vectors of each of a wave's lanes, then up to four of a workgroup's
-// (a wave with eight vectors a lane, 4096 bf16 a row: 2.9 TB/s forward, 1.8 backward; a workgroup with two 4.9 and 4.7); longer rows have kernels of their own (ITEMS = 0).
+// (a wave with eight vectors a lane, 4096 bf16 a row: 2.9 TB/s forward, 1.8 backward; a workgroup with two 5.4 and 5.3).  Longer rows have kernels of their own
+// (ITEMS = 0), which read them again from the caches: 16384 bf16 a row 3.5 and 2.7 TB/s.
 template <typename T, typename Launch> hipError_t ln_spread(int64_t N, bool aligned, Launch launch) {
     constexpr int kVec = kRowVec<T>;
     const auto with = [&](auto even) {
@@ -346,7 +357,7 @@ hipError_t layer_norm_t(const T *x, const T *weight, const T *bias, const int64_
             hipLaunchKernelGGL((layer_norm_long_kernel<T, EVEN>), dim3((unsigned)(all < 4096 ? all : 4096)), dim3(kLnThreads), 0, stream, x, weight, bias, offsets, B, rows, reps, N,
                                eps, y, mean, rstd);
         } else {
-            constexpr int kPerBlock = kLnThreads / L;
+            constexpr int kPerBlock = kLnThreads / L * ln_rows<I>;
             const int64_t need = (rows * reps + kPerBlock - 1) / kPerBlock;
             hipLaunchKernelGGL((layer_norm_kernel<T, I, L, EVEN>), dim3((unsigned)(need < 8192 ? need : 8192)), dim3(kLnThreads), 0, stream, x, weight, bias, offsets, B, rows, reps,
                                (int)N, eps, y, mean, rstd);
