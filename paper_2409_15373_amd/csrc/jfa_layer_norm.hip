@@ -40,62 +40,53 @@ template <typename T, int ITEMS, int LANES, bool EVEN> struct RowPart {
     }
 };
 
-// Rows of the forward that are in flight at a time: two where the lanes of a row have few vectors of it (512 bf16 a row 4.9 -> 5.0 TB/s, 257 fp32 3.4 -> 4.0, 129
-// bf16 2.2 -> 2.6).  The backward's two tensors are enough (5.2 to 5.4 TB/s at 128 to 4096 bf16 a row; reading the next row ahead: 4.4 to 5.0 up to 1024).
-template <int ITEMS> constexpr int ln_rows = ITEMS <= 2 ? 2 : 1;
-
-// LANES lanes per row (a wave or part of one, or the workgroup), ITEMS vectors each, ln_rows rows at a time.
+// LANES lanes per row (a wave or part of one, or the workgroup), ITEMS vectors each, one row at a time.  (Two in flight: 586000 rows of 512 bf16 4.9 -> 5.0 TB/s, but
+// 14848 of them 7.8 -> 8.3 us and 1000 3.0 -> 3.8.)
 template <typename T, int ITEMS, int LANES, bool EVEN>
 __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(const T *__restrict__ x, const T *__restrict__ weight, const T *__restrict__ bias,
                                                                 const int64_t *__restrict__ offsets, int64_t B, int64_t rows, int64_t reps, int N, float eps,
                                                                 T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd) {
-    constexpr int kPerBlock = kLnThreads / LANES, VEC = kRowVec<T>, kRows = ln_rows<ITEMS>;
+    constexpr int kPerBlock = kLnThreads / LANES, VEC = kRowVec<T>;
     __shared__ float slots[4];
-    const int64_t n = rows_there(offsets, B, rows) * reps, step = (int64_t)gridDim.x * kPerBlock * kRows;
+    const int64_t n = rows_there(offsets, B, rows) * reps, step = (int64_t)gridDim.x * kPerBlock;
     const int lane = threadIdx.x % LANES;
     const float inv = 1.0f / (float)N;
-    for (int64_t r0 = (int64_t)blockIdx.x * kPerBlock * kRows + threadIdx.x / LANES; r0 < n; r0 += step) {
-        RowPart<T, ITEMS, LANES, EVEN> part[kRows];
+    RowPart<T, ITEMS, LANES, EVEN> part;
+    for (int64_t r = (int64_t)blockIdx.x * kPerBlock + threadIdx.x / LANES; r < n; r += step) {
+        part.read(x, r, N, lane);
+        float v[ITEMS][VEC], sum = 0.0f;
 #pragma unroll
-        for (int u = 0; u < kRows; ++u) part[u].read(x, r0 + u * kPerBlock < n ? r0 + u * kPerBlock : r0, N, lane);   // (the first again behind the last row)
+        for (int i = 0; i < ITEMS; ++i) {
+            const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
+            widen_vec<T, VEC>(part.v[i], v[i]);
 #pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            const int64_t r = r0 + u * kPerBlock;
-            float v[ITEMS][VEC], sum = 0.0f;
+            for (int e = 0; e < VEC; ++e)
+                if (EVEN || c + e >= own) sum += v[i][e];
+        }
+        const float m = lanes_sum<LANES>(sum, slots) * inv;
+        float square = 0.0f;
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
-                widen_vec<T, VEC>(part[u].v[i], v[i]);
+        for (int i = 0; i < ITEMS; ++i) {
+            const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (EVEN || c + e >= own) sum += v[i][e];
-            }
-            const float m = lanes_sum<LANES>(sum, slots) * inv;
-            float square = 0.0f;
+            for (int e = 0; e < VEC; ++e)
+                if (own < N && (EVEN || (c + e >= own && c + e < N))) square += (v[i][e] - m) * (v[i][e] - m);
+        }
+        const float rs = 1.0f / sqrtf(lanes_sum<LANES>(square, slots) * inv + eps);
+        if (lane == 0) {
+            if (mean) mean[r] = m;
+            if (rstd) rstd[r] = rs;
+        }
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
+        for (int i = 0; i < ITEMS; ++i) {
+            const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
+            if (own < N) {
+                float w[VEC], b[VEC];
+                if (weight) load_vec<T, VEC, EVEN>(weight + c, N - c, w);
+                if (bias) load_vec<T, VEC, EVEN>(bias + c, N - c, b);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (own < N && (EVEN || (c + e >= own && c + e < N))) square += (v[i][e] - m) * (v[i][e] - m);
-            }
-            const float rs = 1.0f / sqrtf(lanes_sum<LANES>(square, slots) * inv + eps);
-            if (kRows > 1 && r >= n) break;
-            if (lane == 0) {
-                if (mean) mean[r] = m;
-                if (rstd) rstd[r] = rs;
-            }
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int own = (i * LANES + lane) * VEC, c = vec_at<VEC, EVEN>(own, N);
-                if (own < N) {
-                    float w[VEC], b[VEC];
-                    if (weight) load_vec<T, VEC, EVEN>(weight + c, N - c, w);
-                    if (bias) load_vec<T, VEC, EVEN>(bias + c, N - c, b);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[i][e] = (v[i][e] - m) * rs * (weight ? w[e] : 1.0f) + (bias ? b[e] : 0.0f);
-                    store_vec<T, VEC, EVEN>(y + r * N + c, N - c, v[i]);
-                }
+                for (int e = 0; e < VEC; ++e) v[i][e] = (v[i][e] - m) * rs * (weight ? w[e] : 1.0f) + (bias ? b[e] : 0.0f);
+                store_vec<T, VEC, EVEN>(y + r * N + c, N - c, v[i]);
             }
         }
     }
@@ -326,7 +317,7 @@ int64_t ln_grid(int64_t rows, int per_block) {
 }
 
 // How a row of N elements of T is spread: up to a wave's lanes with a vector each, then up to four vectors of each of a wave's lanes, then up to four of a workgroup's
-// (a wave with eight vectors a lane, 4096 bf16 a row: 2.9 TB/s forward, 1.8 backward; a workgroup with two 5.4 and 5.3).  Longer rows have kernels of their own
+// (a wave with eight vectors a lane, 4096 bf16 a row: 2.9 TB/s forward, 1.8 backward; a workgroup with two 5.2 and 5.4).  Longer rows have kernels of their own
 // (ITEMS = 0), which read them again from the caches: 16384 bf16 a row 3.5 and 2.7 TB/s.
 template <typename T, typename Launch> hipError_t ln_spread(int64_t N, bool aligned, Launch launch) {
     constexpr int kVec = kRowVec<T>;
@@ -357,7 +348,7 @@ hipError_t layer_norm_t(const T *x, const T *weight, const T *bias, const int64_
             hipLaunchKernelGGL((layer_norm_long_kernel<T, EVEN>), dim3((unsigned)(all < 4096 ? all : 4096)), dim3(kLnThreads), 0, stream, x, weight, bias, offsets, B, rows, reps, N,
                                eps, y, mean, rstd);
         } else {
-            constexpr int kPerBlock = kLnThreads / L * ln_rows<I>;
+            constexpr int kPerBlock = kLnThreads / L;
             const int64_t need = (rows * reps + kPerBlock - 1) / kPerBlock;
             hipLaunchKernelGGL((layer_norm_kernel<T, I, L, EVEN>), dim3((unsigned)(need < 8192 ? need : 8192)), dim3(kLnThreads), 0, stream, x, weight, bias, offsets, B, rows, reps,
                                (int)N, eps, y, mean, rstd);
