@@ -256,8 +256,8 @@ int jfa_jagged_softmax_backward(const void *y, const void *dy, const int64_t *of
  *                        the call's work is done; may be null where that is 0 (pass: 0 = forward, 1 = backward)
  *
  * Products are those of bf16 (or fp32) numbers with fp32 sums; the state is held in fp32.  In the bf16 calls the decayed products of rows up to
- * 64 apart, and the state as a factor of out, are rounded to bf16 in front of their product; a final state (or a gradient of an initial
- * one) is exact to fp32.  A row that is not finite reaches the other rows of its sample and head, earlier ones
+ * 64 apart, and the state as a factor of out, go into their product as the sum of two bf16 numbers (16 bits), so that an output's error is its own
+ * rounding; a final state (or a gradient of an initial one) is exact to fp32.  A row that is not finite reaches the other rows of its sample and head, earlier ones
  * among them, and nothing else.  The gradient of log_decay is not computed.
  * jfa_linear_attention_step takes one row per sequence, q, k, v, out [B, H, D], and a state [B, H, D, D]; new_state may be `state`.
  * At most JFA_LINEAR_MAX_PAIRS samples times heads, H * D at most 2^20.  Everything else as for the calls above.

@@ -70,6 +70,26 @@ def _check_capture():
                                "same leaves is still alive.  Let go of that graph's results first, or run it on the stream of the capture.")
 
 
+class _Once(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tuple(t.detach() for t in tensors[:n])
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the gradients of this operator cannot be differentiated again")
+
+
+def _once(gradients, *of):
+    """A backward's results: where a graph of the backward is being made, going through them to what they were computed from is an error.  (Left as they are
+    they would count as constants.)"""
+    if not torch.is_grad_enabled():
+        return gradients
+    wanted = [g for g in gradients if g is not None]
+    results = iter(_Once.apply(len(wanted), *wanted, *(t for t in of if t is not None)))
+    return tuple(None if g is None else next(results) for g in gradients)
+
+
 class _LinearAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, log_decay, offsets, max_len, scale, initial_state, return_state):
@@ -85,7 +105,7 @@ class _LinearAttention(torch.autograd.Function):
         dq, dk, dv, dinitial = binding.jfa_linear_attention_backward(
             q, k, v, dout.contiguous(), log_decay, offsets, ctx.max_len, ctx.scale, initial_state,
             None if dfinal_state is None else dfinal_state.contiguous(), return_dstate=ctx.needs_input_grad[7])
-        return dq, dk, dv, None, None, None, None, dinitial, None
+        return _once((dq, dk, dv, None, None, None, None, dinitial, None), q, k, v, initial_state, dout, dfinal_state)
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -102,7 +122,7 @@ class _LayerNorm(torch.autograd.Function):
         x, weight, mean, rstd, offsets = ctx.saved_tensors
         dx, dweight, dbias = binding.jfa_layer_norm_backward(x, weight, dy.contiguous(), mean, rstd, offsets, normalized_shape=ctx.shape,
                                                              want_dweight=ctx.needs_input_grad[1], want_dbias=ctx.needs_input_grad[2])
-        return dx, dweight, dbias, None, None
+        return _once((dx, dweight, dbias, None, None), x, weight, dy)
 
 
 class _Embedding(torch.autograd.Function):
@@ -116,7 +136,7 @@ class _Embedding(torch.autograd.Function):
     def backward(ctx, dout):
         _check_capture()
         ids, offsets = ctx.saved_tensors
-        return binding.jfa_embedding_backward(dout.contiguous(), ids, ctx.V, offsets, ctx.scale), None, None, None
+        return _once((binding.jfa_embedding_backward(dout.contiguous(), ids, ctx.V, offsets, ctx.scale), None, None, None), dout)
 
 
 _native = None   # the C++ nodes; False where they have not been built for this torch
@@ -186,8 +206,9 @@ def jagged_flash_cross_attention(q, k, v, offsets_q, offsets_kv, max_len_q: int,
 def jagged_linear_attention(q, k, v, log_decay, offsets, max_len: int, scale=None, initial_state=None, return_state: bool = False):
     """out_i = scale q_i S_i with S_i = exp(log_decay) S_(i-1) + k_i^T v_i per sample and head; q, k, v as for jagged_flash_attention,
     log_decay fp32 [H], scale 1 / sqrt(D) if not given.  initial_state: fp32 [B, H, D, D], zeros if not given; return_state: the samples'
-    final states too, as a second result.  Gradients flow to the states as well, not to log_decay."""
-    if log_decay.requires_grad:
+    final states too, as a second result.  Gradients flow to the states as well, not to log_decay.
+    Of this and the following functions the gradients cannot be differentiated again."""
+    if log_decay.requires_grad and torch.is_grad_enabled():
         raise ValueError("jagged_linear_attention: log_decay is not differentiable")
     args = (q, k, v, log_decay, offsets, int(max_len), q.shape[-1] ** -0.5 if scale is None else float(scale), initial_state, bool(return_state))
     if (nodes := _nodes()) and (result := nodes.linear_attention(*args)) is not None:   # None: not in order, the function below says what is wrong

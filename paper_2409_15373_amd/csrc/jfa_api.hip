@@ -811,7 +811,7 @@ namespace {
 int linear_begin(const char *who, int64_t B, int64_t rows, int64_t max_len, int H, int D) {
     if (B < 0) return fail(JFA_ERR_INVALID_ARG, "%s: B = %lld is negative", who, (long long)B);
     if (max_len < 0 || max_len >= (int64_t)1 << 31) return fail(JFA_ERR_INVALID_ARG, "%s: bad max_len = %lld", who, (long long)max_len);
-    if (rows < 0) return fail(JFA_ERR_INVALID_ARG, "%s: rows = %lld is negative", who, (long long)rows);
+    if (rows < 0 || rows > (int64_t)1 << 38) return fail(JFA_ERR_INVALID_ARG, "%s: bad rows = %lld", who, (long long)rows);   // (segments are counted in 32 bits)
     if (H <= 0) return fail(JFA_ERR_INVALID_ARG, "%s: H = %d must be positive", who, H);
     if (D != 32 && D != 64 && D != 128) return fail(JFA_ERR_UNSUPPORTED, "%s: D = %d is not one of 32, 64, 128", who, D);
     if ((int64_t)H * D > 1 << 20) return fail(JFA_ERR_UNSUPPORTED, "%s: H * D = %lld exceeds 2^20", who, (long long)H * D);   // 32-bit byte offsets inside a chunk

@@ -16,6 +16,8 @@
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <unordered_set>
 
 namespace {
@@ -427,6 +429,15 @@ bool wants_gradient(std::initializer_list<const Tensor *> tensors) {
 }
 Maybe maybe(const Tensor *t) { return t ? Maybe(*t) : Maybe(); }
 
+// A backward's results: where a graph of the backward is being made, going through them to what they were computed from is an error.  (Left as they are they
+// would count as constants.)
+variable_list once(variable_list gradients, const variable_list &from) {
+    if (at::GradMode::is_enabled())
+        torch::autograd::set_history(gradients, std::make_shared<torch::autograd::Error>("the gradients of this operator cannot be differentiated again",
+                                                                                         torch::autograd::collect_next_edges(from)));
+    return gradients;
+}
+
 // (q, k, v, log_decay, offsets, max_len, scale, initial_state) -> out, and the final state if wanted
 std::pair<Tensor, Tensor> linear_call(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay, const Tensor &offsets, int64_t max_len, double scale,
                                       const Maybe &initial, bool want_state) {
@@ -477,7 +488,7 @@ struct LinearAttention : torch::autograd::Function<LinearAttention> {
                                                            (float)ctx->saved_data["scale"].toDouble(), static_cast<float *>(place(saved[5])), static_cast<float *>(place(dfinal)),
                                                            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), static_cast<float *>(place(dinitial)), place(workspace), need, stream()),
                    true);
-        return {dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), dinitial, Tensor()};
+        return once({dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), dinitial, Tensor()}, {q, k, v, saved[5], grads[0], dfinal});
     }
 };
 
@@ -523,7 +534,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
         check_call(lib.norm_backward[type == at::kFloat](x.data_ptr(), place(weight), dy.data_ptr(), mean, mean + rows * reps, static_cast<int64_t *>(place(offsets)),
                                                          call[5] >= 0 ? call[5] - 1 : 0, rows, reps, N, dx.data_ptr(), place(dweight), place(dbias), place(workspace), need, stream()),
                    true);
-        return {dx, dweight, dbias, Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+        return once({dx, dweight, dbias, Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {x, weight, dy});
     }
 };
 
@@ -565,7 +576,7 @@ struct Embedding : torch::autograd::Function<Embedding> {
                                                               call[2] >= 0 ? call[2] - 1 : 0, call[0], V, N, (float)ctx->saved_data["scale"].toDouble(), dtable.data_ptr(),
                                                               place(workspace), need, stream()),
                    true);
-        return {dtable, Tensor(), Tensor(), Tensor()};
+        return once({dtable, Tensor(), Tensor(), Tensor()}, {dout});
     }
 };
 

@@ -131,3 +131,34 @@ def test_tensors_without_rows(dtype):
     out = a.jagged_embedding(table, torch.empty(0, dtype=torch.int64, device="cuda"), off)
     dtable, = torch.autograd.grad(out, table, torch.empty_like(out))
     assert out.shape == (0, 32) and not dtable.any()
+
+
+@pytest.mark.parametrize("which", ["public", "python"])
+@pytest.mark.parametrize("op", OPS)
+def test_gradients_are_not_differentiated(op, which):
+    """A graph of a backward may be made (and equals the gradients without one); what goes through it raises instead of leaving these terms out."""
+    public, python, leaves, douts = setup(op, torch.float32)
+    call = public if which == "public" else python
+    want = results(call, leaves, douts)
+    out = call()
+    outs = out if isinstance(out, tuple) else (out,)
+    douts = tuple(d.clone().requires_grad_() for d in douts)
+    grads = torch.autograd.grad(outs, leaves, douts, create_graph=True)
+    for a, b in zip(grads, want[len(outs):]):
+        assert torch.equal(a, b)
+    loss = sum((g * g).sum() for g in grads) + sum((t * t).sum() for t in leaves)
+    for inputs in (douts,) if op == "embedding" else (leaves, douts):   # (the table's gradient does not depend on the table)
+        with pytest.raises(RuntimeError, match="differentia"):
+            torch.autograd.grad(loss, inputs, retain_graph=True)
+    with pytest.raises(RuntimeError, match="differentia"):
+        loss.backward()
+
+
+def test_decays_that_want_gradients():
+    from paper_2409_15373_amd.autograd import jagged_linear_attention
+    q, k, v = (torch.randn(10, 2, 32, device="cuda") for _ in range(3))
+    decay, off = torch.nn.Parameter(torch.tensor([-0.1, -0.01], device="cuda")), torch.tensor([0, 10], device="cuda")
+    with pytest.raises(ValueError, match="log_decay"):
+        jagged_linear_attention(q, k, v, decay, off, 10)
+    with torch.no_grad():
+        assert torch.equal(jagged_linear_attention(q, k, v, decay, off, 10), jagged_linear_attention(q, k, v, decay.detach(), off, 10))
