@@ -63,6 +63,21 @@ template <> struct Elem<__bf16> {
         for (int e = 0; e < 8; ++e) r[e] = (float)x[e];
         return r;
     }
+    // x rounded; what is left of it stays in x
+    __device__ static Operand take(f32x8 &x) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            bf16x2 pair;
+            pair[0] = (__bf16)x[2 * e];
+            pair[1] = (__bf16)x[2 * e + 1];
+            w[e] = __builtin_bit_cast(uint32_t, pair);
+            asm("" : "+v"(w[e]));   // (else every second element is rounded once more to have it in a register's upper half)
+            x[2 * e] -= __builtin_bit_cast(float, w[e] << 16);
+            x[2 * e + 1] -= __builtin_bit_cast(float, w[e] & 0xffff0000u);
+        }
+        return __builtin_bit_cast(Operand, w);
+    }
     __device__ static void store4(__bf16 *dst, f32x4 x) {
         bf16x4 r;
 #pragma unroll
@@ -100,6 +115,7 @@ template <> struct Elem<float> {
     }
     __device__ static Operand pack(const f32x8 &x) { return x; }
     __device__ static f32x8 widen(Operand x) { return x; }
+    __device__ static Operand take(f32x8 &x) { return x; }
     __device__ static void store4(float *dst, f32x4 x) { *reinterpret_cast<f32x4 *>(dst) = x; }
 };
 
@@ -307,9 +323,7 @@ __global__ __launch_bounds__(2 * D * ROLES * KS, 2) void linear_walk_kernel(Line
                     f32x8 x = eight(p, k * 8);
 #pragma unroll
                     for (int part = 0; part < kSplit; ++part) {
-                        const Operand y = E::pack(x);
-                        put(k, part, y);
-                        if (part + 1 < kSplit) x -= E::widen(y);
+                        put(k, part, part + 1 < kSplit ? E::take(x) : E::pack(x));
                     }
                 }
             };
@@ -392,10 +406,9 @@ __global__ __launch_bounds__(2 * D * ROLES * KS, 2) void linear_walk_kernel(Line
                 f32x8 x = eight(S[ks >> 1], (ks & 1) * 8);
 #pragma unroll
                 for (int part = 0; part < kSplit; ++part) {
-                    const Operand y = E::pack(x);
+                    const Operand y = part + 1 < kSplit ? E::take(x) : E::pack(x);
 #pragma unroll
                     for (int ti = 0; ti < kTiles; ++ti) o[ti] = E::product(y, a[ks & 1][ti], o[ti]);
-                    if (part + 1 < kSplit) x -= E::widen(y);
                 }
             }
             c_is_there();
@@ -518,10 +531,9 @@ __global__ __launch_bounds__(2 * D * ROLES * KS, 2) void linear_walk_kernel(Line
                 for (int e = 0; e < 8; ++e) y[e] *= weight[ks & 1][e];
 #pragma unroll
                 for (int part = 0; part < kParts; ++part) {
-                    const Operand z = E::pack(y);
+                    const Operand z = part + 1 < kParts ? E::take(y) : E::pack(y);
 #pragma unroll
                     for (int m = 0; m < kMine; ++m) S[m] = E::product(x[ks & 1][m], z, S[m]);
-                    if (part + 1 < kParts) y -= E::widen(z);
                 }
             }
         }
