@@ -838,6 +838,7 @@ struct LinearPlan {
     int64_t segment_rows;
     int between;             // states between segments, for each walk and head
     bool ordered;            // longest samples first
+    bool few;                // all rows take no longer than the longest sample's walk
     bool apart;              // the backward's three walks in workgroups of their own
     int64_t order_words, bytes;   // of the workspace: the order, all of it
 };

@@ -142,9 +142,10 @@ __device__ inline int64_t state_between(int walk, int h, int H, int between, int
 
 }  // namespace
 
-// A workgroup takes one (sample, head, segment), blockIdx.x, through ROLES walks that go the same way over the same tensors: one of them (walk
-// blockIdx.y), or the two that give dk and dv, which share the tiles of q and dout.  Each walk has D / 32 waves, each of which owns 32 columns of
-// the state and of the outputs.
+// A workgroup takes one (sample, head, segment) through ROLES walks that go the same way over the same tensors: one of them, or the two that
+// give dk and dv, which share the tiles of q and dout.  Each walk has D / 32 waves, each of which owns 32 columns of the state and of the outputs.
+// Workgroups go to the eight dies in turn.  ROLES = 1: the `sides` walks of a (sample, head, segment) follow each other on one die, whose L2 then has the tensors that
+// they share (1024 x 4 heads of up to 1024 rows, D = 128, three walks: 1518 -> 1370 us, 1024 samples of 64 rows 52 -> 40; one walk after another 1500).
 // KS = 2 (one walk; D = 64, and fp32 at D = 128): twice as many waves, two to a strip of 32 columns with half of the state's rows each; out is summed over
 // the two halves through LDS.  Where few walks run, what a chunk takes is the issue of one wave's instructions.  fp32: the fp32 matrix instructions,
 // 64 clocks for 4096 products, are what a chunk waits for: 48 of them for a wave instead of 112 (D = 128: 80 of 208); there P, too, is a sum over the waves, a
@@ -158,7 +159,7 @@ __device__ inline int64_t state_between(int walk, int h, int H, int between, int
 template <typename T, int D, int ROLES, int KS, int kParts, bool kStateOnly>
 __global__ __launch_bounds__(2 * D * ROLES * KS, 2) void linear_walk_kernel(LinearWalks walks, const float *__restrict__ log_decay, const int64_t *__restrict__ offsets,
                                                                        const int32_t *__restrict__ order, int B, int H, int segments, int segment_rows, int between,
-                                                                       float *__restrict__ carried) {
+                                                                       int sides, float *__restrict__ carried) {
     typedef Elem<T> E;
     typedef typename E::Operand Operand;
     constexpr int kRows = E::kRows, kSize = (int)sizeof(T), kStateTiles = D / 32, kSteps = D / 16, kSplit = E::kSplit;
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(2 * D * ROLES * KS, 2) void linear_walk_kernel(Line
     constexpr int kChunks = D * kSize / 16, kTileBytes = kRows * kChunks * 16, kLoads = kRows * kChunks / (64 * kWaves);   // 16-byte chunks of a row; copies of a tile per wave
     // Places of tiles.  A is free for the next chunk's once the state's product with it is done, in the middle of a chunk.  B and, of two walks, C (their B
     // and C change places) are read to the end: there are two of each, the next chunk's fetched from the start of a chunk on.  One walk's C is fetched when the
-    // chunk before is done, which is in time for the products with it.  So two workgroups have room on a compute unit (D = 128, two walks: one).
+    // chunk before is done, which is in time for the products with it.  So two workgroups have room on a compute unit.
     constexpr int kPlaces = ROLES == 2 ? 6 : 4;
     // P: its tiles are shared out among a walk's waves, which leave them as operands, 16 bytes per lane; a single wave (and the fp32 kernels, whose P is
     // one tile) has it in registers.
@@ -184,13 +185,14 @@ __global__ __launch_bounds__(2 * D * ROLES * KS, 2) void linear_walk_kernel(Line
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int role = wave / kWalkWaves, walk_wave = wave % kWalkWaves, strip = walk_wave % kStateTiles, part = walk_wave / kStateTiles;
     const int col = lane & 31, half = lane >> 5;
-    const int which = ROLES == 2 ? 1 : (int)blockIdx.y;   // the first role's walk
+    const int which = ROLES == 2 ? 1 : (int)(blockIdx.x / 8) % sides + (int)blockIdx.y;   // the first role's walk
     const LinearWalk &walk = walks.walk[which + role];
-    // Workgroups go to the eight dies in turn.  Heads that share 128-byte lines are for one of them, whose L2 reads a line once (600 rows x 512 x 4, D = 32: 103 -> 67 us).
+    const int block = ROLES == 2 ? (int)blockIdx.x : (int)(blockIdx.x / (8 * sides)) * 8 + (int)(blockIdx.x % 8);
+    // Heads that share 128-byte lines are for one die, whose L2 reads a line once (600 rows x 512 x 4, D = 32: 103 -> 67 us).
     constexpr bool kSameDie = D * sizeof(T) < 128;
-    const int at = kSameDie ? (int)(blockIdx.x / (8 * H)) * 8 + (int)(blockIdx.x % 8) : (int)(blockIdx.x / H), h = kSameDie ? (int)(blockIdx.x / 8) % H : (int)(blockIdx.x % H);
+    const int at = kSameDie ? block / (8 * H) * 8 + block % 8 : block / H, h = kSameDie ? block / 8 % H : block % H;
     const int at_sample = at / segments, segment = at - at_sample * segments;
-    if (kSameDie && at_sample >= B) return;
+    if (at_sample >= B) return;
     const int b = order ? order[at_sample] : at_sample, pair = b * H + h;
     const int64_t first = offsets[b];
     const int64_t L = offsets[b + 1] - first;
@@ -626,8 +628,9 @@ __global__ __launch_bounds__(256) void linear_step_kernel(const T *__restrict__ 
 // the two passes over a segment.  8 x 2 samples of up to 16000 rows (D = 128) otherwise: 250 chunks one after the other.
 // Many samples of different lengths that are not cut are walked longest first: the walks that are left at the end are short ones (512 x 4 samples of up to 1024
 // rows, forward 307 -> 260 us); the order is made by the attention's scheduler.
-// The backward's three walks are three workgroups where all of their rows take no longer than the longest sample's walk; else dk and dv are one, which reads 6 tensors
-// instead of 8 (64 samples of 600 rows, D = 64, fp32 161 -> 58 us, bf16 62 -> 32).  fp32 at D = 128: three, two have no room on a compute unit.
+// The backward's three walks are three workgroups, side by side (see linear_walk_kernel).  At D = 64 and with many rows (W >= 1024) two: there dk and dv as one, which
+// reads 6 tensors instead of 8, are faster (1024 x 8 heads of up to 1024 rows: 1390 us and three 1465; fp32, 4 heads, 1790 and 1870; but 512 samples of 256 rows,
+// W = 256, 41.5 and three 39.5, 256 of 64 rows 11.0 and 7.5).  few: where all rows take no longer than the longest sample's walk.
 LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, bool backward) {
     constexpr int64_t kPlaces = 2 * 256, kLeastSegment = 256, kMostSegment = 1024;
     LinearPlan p;
@@ -645,43 +648,51 @@ LinearPlan linear_plan(int64_t B, int64_t rows, int64_t max_len, int H, int D, b
             p.between = (int)(rows / segment);
         }
     }
-    p.apart = 3 * W < max_len;
+    p.few = 3 * W < max_len;
+    p.apart = D != 64 || p.few || W < 1024;
     p.ordered = p.segments == 1 && B > 1 && B * H > kPlaces && max_len >= 512 && (double)max_len * B > 1.2 * rows;
     p.order_words = p.ordered ? (2 * B + 1 + kNumCounters + 63) / 64 * 64 : 0;
     p.bytes = p.order_words * 4 + (int64_t)(backward ? 2 : 1) * H * p.between * D * D * 4;
     return p;
 }
 
-template <typename T, int D, int KS, int kParts>
+template <typename T, int D, int KS, int kParts, bool kStateOnly>
+static void launch_side_by_side(const LinearWalks &walks, int n, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H, const LinearPlan &p,
+                                float *carried, hipStream_t stream) {
+    constexpr unsigned kThreads = 2 * D * KS;
+    const int64_t blocks = D * sizeof(T) < 128 ? (B * p.segments + 7) / 8 * 8 * H : (B * p.segments * H + 7) / 8 * 8;
+    const bool fit = n * blocks * kThreads < (int64_t)1 << 32;   // (what a launch has room for in x)
+    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, KS, kParts, kStateOnly>), dim3((unsigned)(fit ? n * blocks : blocks), fit ? 1 : n), dim3(kThreads), 0, stream, walks, log_decay,
+                       offsets, order, (int)B, H, p.segments, (int)p.segment_rows, p.between, fit ? n : 1, carried);
+}
+template <typename T, int D, int kParts>
 static void launch_walks(const LinearWalks &walks, bool backward, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H, const LinearPlan &p,
                          float *carried, hipStream_t stream) {
-    const int segments = p.segments, segment_rows = (int)p.segment_rows, between = p.between;
-    const unsigned blocks = (unsigned)((D * sizeof(T) < 128 ? (B * segments + 7) / 8 * 8 : B * segments) * H);
-    constexpr int kThreads = 2 * D * KS;
-    if (segments > 1) {   // walk 0, and of the two that go back, which have one state, walk 2
+    constexpr int KS = D == 64 || (D == 128 && sizeof(T) == 4) ? 2 : 1;
+    if (p.segments > 1) {   // walk 0, and of the two that go back, which have one state, walk 2
         const LinearWalks states{{walks.walk[0], walks.walk[2], walks.walk[2]}};
         const int n = backward ? 2 : 1;
-        hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, KS, kParts, true>), dim3(blocks, n), dim3(kThreads), 0, stream, states, log_decay, offsets, order, (int)B, H, segments,
-                           segment_rows, between, carried);
-        hipLaunchKernelGGL(linear_carry_kernel, dim3((unsigned)(B * H * (D * D / 1024)), n), dim3(256), 0, stream, states, log_decay, offsets, H, D, segments, segment_rows,
-                           between, carried);
+        launch_side_by_side<T, D, KS, kParts, true>(states, n, log_decay, offsets, order, B, H, p, carried, stream);
+        hipLaunchKernelGGL(linear_carry_kernel, dim3((unsigned)(B * H * (D * D / 1024)), n), dim3(256), 0, stream, states, log_decay, offsets, H, D, p.segments, (int)p.segment_rows,
+                           p.between, carried);
     }
-    constexpr bool kTwo = sizeof(T) == 2 || D < 128;   // (fp32 at D = 128: two walks have no room on a compute unit)
-    const bool apart = p.apart || !kTwo;
-    hipLaunchKernelGGL((linear_walk_kernel<T, D, 1, KS, kParts, false>), dim3(blocks, backward && apart ? 3 : 1), dim3(kThreads), 0, stream, walks, log_decay, offsets, order, (int)B, H,
-                       segments, segment_rows, between, carried);
-    if constexpr (kTwo)
+    const bool apart = backward && p.apart;
+    // (bf16, D = 64, three walks of many rows: 512 samples of 256 rows 39.5 us with two waves a walk, 43 with four)
+    if (D == 64 && sizeof(T) == 2 && apart && !p.few)
+        launch_side_by_side<T, D, 1, kParts, false>(walks, 3, log_decay, offsets, order, B, H, p, carried, stream);
+    else
+        launch_side_by_side<T, D, KS, kParts, false>(walks, apart ? 3 : 1, log_decay, offsets, order, B, H, p, carried, stream);
+    if constexpr (D == 64)
         if (backward && !apart)
-            hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, 1, kParts, false>), dim3(blocks), dim3(4 * D), 0, stream, walks, log_decay, offsets, order, (int)B, H, segments, segment_rows,
-                               between, carried);
+            hipLaunchKernelGGL((linear_walk_kernel<T, D, 2, 1, kParts, false>), dim3((unsigned)(B * p.segments * H)), dim3(4 * D), 0, stream, walks, log_decay, offsets, order, (int)B,
+                               H, p.segments, (int)p.segment_rows, p.between, 1, carried);
 }
 template <typename T, int D>
 static hipError_t launch_walks(const LinearWalks &walks, bool backward, bool states, const float *log_decay, const int64_t *offsets, const int32_t *order, int64_t B, int H,
                                const LinearPlan &p, float *carried, hipStream_t stream) {
-    constexpr int KS = D == 64 || (D == 128 && sizeof(T) == 4) ? 2 : 1;
-    if constexpr (sizeof(T) == 4) launch_walks<T, D, KS, 1>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
-    else if (states) launch_walks<T, D, KS, 3>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
-    else launch_walks<T, D, KS, 2>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
+    if constexpr (sizeof(T) == 4) launch_walks<T, D, 1>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
+    else if (states) launch_walks<T, D, 3>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
+    else launch_walks<T, D, 2>(walks, backward, log_decay, offsets, order, B, H, p, carried, stream);
     return hipGetLastError();
 }
 
