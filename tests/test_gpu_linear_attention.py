@@ -156,6 +156,19 @@ def test_many_samples_longest_first(dtype):
     case.check_backward()
 
 
+@pytest.mark.parametrize("states", [False, True])
+@pytest.mark.parametrize("room", [20000, 270000])
+@pytest.mark.parametrize("D", [32, 64])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_enough_for_other_walks(dtype, D, room, states):
+    """The backward's walks are laid out by the number of rows (the tensors' own, with the room behind the samples): not few, and many."""
+    case = Case(LENGTHS, 2, D, dtype, seed=room + D, states=states)
+    for name in ("q", "k", "v", "dout"):
+        case.t[name] = torch.cat([case.t[name], torch.full((room, 2, D), float("nan"), dtype=dtype, device="cuda")])
+    case.check_forward()
+    case.check_backward()
+
+
 @pytest.mark.parametrize("max_len", [200, 4000, 100000])
 def test_the_bound_on_the_lengths_only_chooses_the_segments(max_len):
     """Results within rounding of one another whatever bound on the lengths is given."""
