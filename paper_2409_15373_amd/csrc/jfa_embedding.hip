@@ -16,7 +16,6 @@ namespace jfa {
 namespace {
 
 constexpr int kEmThreads = 256;
-constexpr int kEmTile = 4096;    // positions that a workgroup sorts at a time (2048: 20000 ids 44 -> 40 us, but 322248 of 1000003 102 -> 116)
 constexpr int kEmBlock = 32;     // sorted positions of a block
 constexpr int kEmSuper = 64;     // blocks that are added at once
 constexpr int kEmMostBits = 10;  // of a sort's digit
@@ -90,8 +89,8 @@ __device__ inline void clear_share(const Clearing &c, int64_t unit) {
     for (int64_t i = at + threadIdx.x * 2; i < at + kClearBytes && i < c.bytes; i += kSortThreads * 2) *reinterpret_cast<uint16_t *>(c.dst + i) = 0;
 }
 
-// counts[tile][bin].
-template <bool FIRST>
+// counts[tile][bin].  TILE: positions that a workgroup sorts at a time.
+template <bool FIRST, int TILE>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortSource s, int shift, int bits, int tiles, uint32_t *__restrict__ counts, Clearing clearing) {
     __shared__ uint32_t bins[1 << kEmMostBits];
     if ((int)blockIdx.x >= tiles) return clear_share(clearing, clearing.from + blockIdx.x - tiles);
@@ -99,7 +98,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortSource s, 
     for (int i = threadIdx.x; i < n_bins; i += kSortThreads) bins[i] = 0;
     __syncthreads();
     const int64_t there = FIRST ? rows_there(s.offsets, s.B, s.rows) : 0;
-    const int first = (int)blockIdx.x * kEmTile, end = s.rows - first < kEmTile ? s.rows : first + kEmTile;
+    const int first = (int)blockIdx.x * TILE, end = s.rows - first < TILE ? s.rows : first + TILE;
     for (int i = first + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&bins[(sort_key<FIRST>(s, there, i) >> shift) & (n_bins - 1)], 1u);
     __syncthreads();
     for (int i = threadIdx.x; i < n_bins; i += kSortThreads) counts[(int64_t)blockIdx.x * n_bins + i] = bins[i];
@@ -136,13 +135,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(int n_bins, int
 }
 
 // Every key and position to its place.  A wave has a sixteenth of the tile in order; equal digits of a wave's 64 keys are ranked by ballots.
-// totals: null where nobody has scanned the counts.  Up to kFewTiles tiles a workgroup adds its bins' counts itself, in less time than a launch takes.
-constexpr int kFewTiles = 128;
-template <bool FIRST>
+// totals: null where nobody has scanned the counts.  Up to kFewTiles tiles a workgroup adds its bins' counts itself, in less time than a launch takes
+// (64 tiles, 131072 rows: 64 us, with a launch 69; 79 tiles of 4096, 322248 rows: 102 and 92).
+constexpr int kFewTiles = 64;
+template <bool FIRST, int TILE>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, int shift, int bits, int tiles, const uint32_t *__restrict__ counts,
                                                                   const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys, uint32_t *__restrict__ positions,
                                                                   Clearing clearing) {
-    constexpr int kWaves = kSortThreads / 64, kMine = kEmTile / kWaves, kRounds = kMine / 64;
+    constexpr int kWaves = kSortThreads / 64, kMine = TILE / kWaves, kRounds = kMine / 64;
     __shared__ uint32_t next[kWaves][1 << kEmMostBits];
     __shared__ uint32_t wave_totals[kWaves];
     if ((int)blockIdx.x >= tiles) return clear_share(clearing, clearing.from + blockIdx.x - tiles);
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortSource s, 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t there = FIRST ? rows_there(s.offsets, s.B, s.rows) : 0;
     for (int i = threadIdx.x; i < n_bins * kWaves; i += kSortThreads) next[i >> bits][i & mask] = 0;
-    const int first = (int)blockIdx.x * kEmTile + wave * kMine;
+    const int first = (int)blockIdx.x * TILE + wave * kMine;
     uint32_t key[kRounds], position[kRounds];
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
@@ -465,17 +465,20 @@ hipError_t embedding_t(const T *table, const Id *ids, const int64_t *offsets, in
 
 // The workspace's parts, in 4-byte words from its start.
 struct EmPlan {
-    int bits, passes, tiles;
+    int bits, passes, tile, tiles;
     int n_blocks, n_supers;
     int64_t counts, totals, keys[2], positions[2], heads, tails, supers, words;
 };
 EmPlan em_plan(int64_t rows, int64_t V, int64_t N) {
     EmPlan p;
+    // One tile where they fit (2000 rows: 24.4 us with a tile of 2048, 27.7 with two of 1024); up to kFewTiles tiles small ones, which put more compute units to work (20000 rows,
+    // 1024, 2048 and 4096: 34.5, 39.8 and 44.0 us; 322248: 92, 87 and 92); many rows large ones, with fewer counts (2000000: 222, 198 and 184).
+    p.tile = rows <= 1024 ? 1024 : rows <= 2048 ? 2048 : rows <= kFewTiles * 1024 ? 1024 : rows <= 1 << 19 ? 2048 : 4096;
     int bits = 1;
     while (((int64_t)1 << bits) < V + 1) ++bits;   // keys 0 .. V
     p.passes = (bits + kEmMostBits - 1) / kEmMostBits;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.tiles = (int)((rows + kEmTile - 1) / kEmTile);
+    p.tiles = (int)((rows + p.tile - 1) / p.tile);
     p.n_blocks = (int)((rows + kEmBlock - 1) / kEmBlock);
     p.n_supers = (int)(rows / (kEmBlock * kEmSuper));
     int64_t at = 0;
@@ -510,27 +513,34 @@ hipError_t embedding_backward_t(const T *dout, const void *ids, bool ids64, cons
     const auto grid = [](int own, const Clearing &c) { return dim3((unsigned)(own + c.to - c.from)); };
     if (rows == 0) {
         const Clearing c{(char *)dtable, table_bytes, 0, units};
-        hipLaunchKernelGGL((sort_count_kernel<true>), grid(0, c), threads, 0, stream, s, 0, 1, 0, nullptr, c);
+        hipLaunchKernelGGL((sort_count_kernel<true, 1024>), grid(0, c), threads, 0, stream, s, 0, 1, 0, nullptr, c);
         return hipGetLastError();
     }
-    for (int pass = 0; pass < p.passes; ++pass) {
-        uint32_t *const keys = ws + p.keys[pass & 1], *const positions = ws + p.positions[pass & 1];
-        const int shift = pass * p.bits, bins = 1 << p.bits;
+    const auto pass = [&](auto first, auto tile, int number) {
+        constexpr bool FIRST = decltype(first)::value;
+        constexpr int TILE = decltype(tile)::value;
+        uint32_t *const keys = ws + p.keys[number & 1], *const positions = ws + p.positions[number & 1];
+        const int shift = number * p.bits, bins = 1 << p.bits;
         if (p.tiles > 1) {
             const Clearing c = share();
-            if (pass == 0) hipLaunchKernelGGL((sort_count_kernel<true>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, c);
-            else hipLaunchKernelGGL((sort_count_kernel<false>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, c);
+            hipLaunchKernelGGL((sort_count_kernel<FIRST, TILE>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, c);
         }
         if (scan) {
             const Clearing c = share();
             hipLaunchKernelGGL(sort_scan_kernel, grid((bins + 63) / 64, c), threads, 0, stream, bins, p.tiles, counts, totals, c);
         }
         const Clearing c = share();
-        if (pass == 0) hipLaunchKernelGGL((sort_place_kernel<true>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions, c);
-        else hipLaunchKernelGGL((sort_place_kernel<false>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions, c);
+        hipLaunchKernelGGL((sort_place_kernel<FIRST, TILE>), grid(p.tiles, c), threads, 0, stream, s, shift, p.bits, p.tiles, counts, totals, keys, positions, c);
         s.keys = keys;
         s.positions = positions;
-    }
+    };
+    const auto sort = [&](auto tile) {
+        pass(std::true_type{}, tile, 0);
+        for (int number = 1; number < p.passes; ++number) pass(std::false_type{}, tile, number);
+    };
+    if (p.tile == 1024) sort(std::integral_constant<int, 1024>{});
+    else if (p.tile == 2048) sort(std::integral_constant<int, 2048>{});
+    else sort(std::integral_constant<int, 4096>{});
     float *const heads = reinterpret_cast<float *>(ws + p.heads), *const tails = reinterpret_cast<float *>(ws + p.tails), *const supers = reinterpret_cast<float *>(ws + p.supers);
     return em_spread<T>(N, aligned16(dout, dtable), [&](auto even, auto lanes) {
         constexpr bool EVEN = decltype(even)::value;

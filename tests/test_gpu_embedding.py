@@ -69,6 +69,19 @@ def test_row_and_table_sizes(V, rows):
     check(table, ids, dout, 1.5, *both(table, ids, dout))
 
 
+@pytest.mark.parametrize("rows", [1023, 1024, 1025, 2047, 2048, 2049, 65535, 65536, 65537, 131073, 524288, 524289])
+@pytest.mark.parametrize("V", [900, 5000])
+def test_where_the_sort_changes_its_tiles(V, rows):
+    from paper_2409_15373_amd import binding
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    ids = torch.randint(-1, V + 1, (rows,), device="cuda", generator=gen)
+    ids[::7] = V // 2
+    dout = torch.randint(-8, 9, (rows, 8), device="cuda", generator=gen).float()   # whole numbers: sums are exact
+    inside = (ids >= 0) & (ids < V)
+    want = torch.zeros(V, 8, device="cuda", dtype=torch.float64).index_add_(0, ids[inside], dout[inside].double())
+    assert torch.equal(binding.jfa_embedding_backward(dout, ids, V).double(), want)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V", [3, 1100000])
 def test_frequent_ids(dtype, V):

@@ -138,3 +138,10 @@ def test_tensors_that_are_not_on_a_gpu_are_refused():
         autograd.jagged_embedding(x, torch.arange(8))
     with pytest.raises(ValueError):
         autograd.jagged_linear_attention(x, x, x, decay.requires_grad_(), offsets, 8)
+
+
+def test_linear_attention_of_more_rows_than_there_can_be(lib):
+    assert lib.jfa_linear_attention_workspace_bytes(1, 1 << 38, 5, 1, 32, 0) == 0   # none needed
+    refused(lib.jfa_linear_attention(16, 16, 16, 16, 16, 1, (1 << 38) + 1, 5, 1, 32, 1.0, None, 16, None, None, 0, None), BAD, "rows")
+    assert lib.jfa_linear_attention_workspace_bytes(1, (1 << 38) + 1, 5, 1, 32, 0) == 0
+    assert "rows" in binding.jfa_last_error()
