@@ -14,6 +14,7 @@ step on a small batch spends half as much host time in; the torch.autograd.Funct
 
 q, k, v: [rows, H, D] bf16 or fp32 on the GPU, contiguous; offsets: int64 [B + 1] on the GPU.  Gradients flow to q, k
 and v (and to x, weight, bias, the table and the states); offsets, ids, decays and the length bounds are not differentiable.
+Rows behind offsets[B] are nobody's: they are not read, and results and gradients hold anything there.
 """
 import ctypes
 import importlib.util
