@@ -113,3 +113,57 @@ def test_a_captured_training_step():
         torch.cuda.synchronize()
         assert torch.equal(again[0], alive) and all(torch.equal(a, b) for a, b in zip(again[1], eager))
         assert torch.equal(out, alive) and all(torch.equal(a, b) for a, b in zip(grads, eager))
+
+
+def test_two_streams_at_once():
+    """Two batches' steps on a stream each, with no wait between them; the first call waits so that the others overlap."""
+    blocks = [Block([300, 40, 0, 200], 50, 2, 64, torch.float32, seed) for seed in (1, 2)]
+    want = [block.ours(False) for block in blocks]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for stream in streams:
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(20_000_000)
+    got = [[], []]
+    for _ in range(3):
+        for i, (block, stream) in enumerate(zip(blocks, streams)):
+            with torch.cuda.stream(stream):
+                got[i].append(block.ours(False))
+    torch.cuda.synchronize()
+    for results, expected in zip(got, want):
+        for result in results:
+            assert all(torch.equal(a, b) for a, b in zip(result, expected))
+
+
+def test_two_graphs_replayed_at_once():
+    """The gradients' calls, captured into two graphs with workspaces of their own, replayed on two streams at a time."""
+    from paper_2409_15373_amd import binding
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    offsets = torch.tensor([0, 1500, 1500, 1503], device="cuda")
+    decay, ids = torch.tensor([-0.01], device="cuda"), torch.randint(0, 5000, (1503,), device="cuda", generator=gen)
+    w = torch.ones(64, device="cuda")
+
+    def calls(t):
+        norm = binding.jfa_layer_norm(t[0].view(-1, 64), w, w, offsets)
+        return (*binding.jfa_linear_attention_backward(*t, decay, offsets, 1500)[:3], *binding.jfa_layer_norm_backward(t[0].view(-1, 64), w, t[1].view(-1, 64), norm[1], norm[2], offsets),
+                binding.jfa_embedding_backward(t[0].view(-1, 64), ids, 5000, offsets))
+    tensors = [[torch.randn(1503, 1, 64, device="cuda", generator=gen) for _ in range(4)] for _ in range(2)]
+    want = [calls(t) for t in tensors]
+    graphs, results = [], []
+    for t in tensors:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            results.append(calls(t))
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(4):
+        for result in results:
+            for x in result:
+                x.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for result, expected in zip(results, want):
+            assert all(torch.equal(a, b) for a, b in zip(result, expected))
